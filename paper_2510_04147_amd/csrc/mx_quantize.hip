@@ -1,0 +1,220 @@
+// Microscaled quantisation, and RMSNorm with an 8-bit output.
+#include "../../include/ssd_mx.h"
+#include "mx.h"
+
+__device__ __forceinline__ void mx_load8(const float* p, float* v) {
+    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void mx_load8(const bf16_t* p, float* v) {
+    const uint4 a = *(const uint4*)p;
+    const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void mx_store8(float* p, const float* v) {
+    ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void mx_store8(bf16_t* p, const float* v) {      // rounded values have at most four significant bits
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
+    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The other lanes' values, by DPP: lane ^ 1, lane ^ 2; then of the other four lanes of eight, the other eight of sixteen.
+template <int CTRL>
+__device__ __forceinline__ unsigned mx_dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ unsigned mx_max(unsigned a, unsigned b) { return a > b ? a : b; }
+
+// Quantisation.  A work-group of four waves takes 32 rows x 512 columns: a wave reads 512 columns of a row in one go, eight values
+// to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has its eight rows' loads in flight together.
+// The tile's scale words meet in LDS and leave as whole lines.  Reads every value once: bound by memory.
+template <typename T, int BITS, bool VALUES>
+__global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, int rows, int cols, uint8_t* __restrict__ codes,
+                                                     uint32_t* __restrict__ scales, T* __restrict__ values) {
+    __shared__ uint32_t words[4][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row0 = blockIdx.x * 32, col = blockIdx.y * 512 + lane * 8;
+    const bool in = col < cols;                              // whole blocks are in or out
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = row0 + wave * 8 + i;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        if (in && row < rows) mx_load8(src + (size_t)row * cols + col, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = row0 + wave * 8 + i;
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = mx_max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+        top = mx_max(top, mx_dpp<0xB1>(top));
+        top = mx_max(top, mx_dpp<0x4E>(top));
+        unsigned code = mx_scale_code<BITS>(top);
+        const float scale = mx_scale_value(code);
+        if (code == 255)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        if (in && row < rows) {
+            const size_t at = (size_t)row * cols + col;
+            if constexpr (BITS == 4) {
+                const unsigned o = mx_pack4(v[i], scale);
+                *(uint32_t*)(codes + at / 2) = o;
+                if constexpr (VALUES) {
+                    float r[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        // sign, two bits of exponent, one of mantissa, to a float: the exponent in place, or half the mantissa
+                        const unsigned c = o >> (4 * j), e = c >> 1 & 3, m = c & 1;
+                        const float mag = e ? __uint_as_float((126 + e) << 23 | m << 22) : m * 0.5f;
+                        r[j] = code == 255 ? NAN : (c & 8 ? -mag : mag) * scale;
+                    }
+                    mx_store8(values + at, r);
+                }
+            } else {
+                const unsigned a = mx_pack8(v[i], scale), b = mx_pack8(v[i] + 4, scale);
+                *(uint2*)(codes + at) = make_uint2(a, b);
+                if constexpr (VALUES) {
+                    float r[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const unsigned c = (j < 4 ? a : b) >> (8 * (j & 3)), e = c >> 3 & 15, m = c & 7;
+                        const float mag = e ? __uint_as_float((120 + e) << 23 | m << 20) : m * 0x1p-9f;
+                        r[j] = code == 255 ? NAN : (c & 128 ? -mag : mag) * scale;
+                    }
+                    mx_store8(values + at, r);
+                }
+            }
+        }
+        if (!in || row >= rows) code = 127;                  // what only fills up
+        // the word: four blocks of four lanes
+        unsigned word = code << ((lane >> 2 & 3) * 8);
+        word |= mx_dpp<0x141>(word);
+        word |= mx_dpp<0x140>(word);
+        if ((lane & 15) == 0) words[lane >> 4][wave * 8 + i] = word;
+    }
+    __syncthreads();
+    const int group = blockIdx.y * 4 + (threadIdx.x >> 5);
+    if (threadIdx.x < 128 && group < mx_groups(cols)) scales[(size_t)group * mx_pad_rows(rows) + row0 + (threadIdx.x & 31)] = words[threadIdx.x >> 5][threadIdx.x & 31];
+}
+
+void mx_launch_quantize(const void* src, int dtype, int rows, int cols, int format, void* codes, void* scales, void* values, hipStream_t st) {
+    const dim3 grid((rows + 31) / 32, (cols + 511) / 512);
+    auto run = [&](auto t, auto bits, auto with) {
+        using T = decltype(t);
+        k_mx_quantize<T, decltype(bits)::value, decltype(with)::value><<<grid, 256, 0, st>>>((const T*)src, rows, cols, (uint8_t*)codes, (uint32_t*)scales, (T*)values);
+    };
+    auto typed = [&](auto t) {
+        if (format == SSD_MX_FP4) values ? run(t, std::integral_constant<int, 4>{}, std::true_type{}) : run(t, std::integral_constant<int, 4>{}, std::false_type{});
+        else values ? run(t, std::integral_constant<int, 8>{}, std::true_type{}) : run(t, std::integral_constant<int, 8>{}, std::false_type{});
+    };
+    if (dtype == SSD_F32) typed(0.f);
+    else typed(bf16_t(0));
+}
+
+// RMSNorm behind the residual's addition, output in 8 bits.  One work-group per row, four values to a lane: a block is eight lanes, a
+// scale word 32.  The row and all its partial sums are in flight at once; the row stays in registers between the two passes over it
+// (mean square, then scale and conversion).
+#define MX_NORM_T 1024
+#define MX_NORM_J 2
+template <int NP>
+__device__ __forceinline__ float4 mx_sum_partials(float4 v, const float* p, size_t stride, int i4) {
+    // the first half's sum, then the second's
+    auto add = [](float4& x, const float4& y) { x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; };
+    float4 pv[NP > 0 ? NP : 1];
+#pragma unroll
+    for (int s = 0; s < NP; ++s) pv[s] = ((const float4*)(p + s * stride))[i4];
+    constexpr int HALF = (NP + 1) / 2;
+    if constexpr (NP > 0) {
+        float4 t = pv[0];
+#pragma unroll
+        for (int s = 1; s < HALF; ++s) add(t, pv[s]);
+        add(v, t);
+    }
+    if constexpr (NP > 1) {
+        float4 t = pv[HALF];
+#pragma unroll
+        for (int s = HALF + 1; s < NP; ++s) add(t, pv[s]);
+        add(v, t);
+    }
+    return v;
+}
+
+template <int NP>
+__global__ __launch_bounds__(MX_NORM_T) void k_mx_norm(const float* h, const float* part, size_t part_stride, const float* gain, float eps, int rows,
+                                                      int cols, float* h_out, uint8_t* codes, uint32_t* scales) {
+    const int row = blockIdx.x, n4 = cols >> 2, lane = threadIdx.x & 63;
+    const size_t at = (size_t)row * cols;
+    float4 v[MX_NORM_J], g[MX_NORM_J];
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < MX_NORM_J; ++j) {
+        const int i4 = threadIdx.x + j * MX_NORM_T;
+        v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i4 < n4) {
+            v[j] = ((const float4*)(h + at))[i4];
+            g[j] = ((const float4*)gain)[i4];
+            v[j] = mx_sum_partials<NP>(v[j], part + at, part_stride, i4);
+            if (h_out && (NP > 0 || h_out != h)) ((float4*)(h_out + at))[i4] = v[j];
+            ss += v[j].x * v[j].x + v[j].y * v[j].y + v[j].z * v[j].z + v[j].w * v[j].w;
+        }
+    }
+    __shared__ float red[MX_NORM_T / 64];
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) ss += __shfl_xor(ss, s);
+    if (lane == 0) red[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    float tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < MX_NORM_T / 64; ++w) tot += red[w];
+    const float r = 1.0f / sqrtf(tot / (float)cols + eps);
+    const int groups = mx_groups(cols), pad = mx_pad_rows(rows);
+#pragma unroll
+    for (int j = 0; j < MX_NORM_J; ++j) {
+        const int i4 = threadIdx.x + j * MX_NORM_T;
+        const bool in = i4 < n4;
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        if (in) { y[0] = v[j].x * r * g[j].x; y[1] = v[j].y * r * g[j].y; y[2] = v[j].z * r * g[j].z; y[3] = v[j].w * r * g[j].w; }
+        unsigned top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = mx_max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+        top = mx_max(top, mx_dpp<0xB1>(top));
+        top = mx_max(top, mx_dpp<0x4E>(top));
+        top = mx_max(top, mx_dpp<0x141>(top));
+        unsigned code = mx_scale_code<8>(top);
+        if (code == 255)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = 0.f;
+        if (in) *(uint32_t*)(codes + at + 4 * i4) = mx_pack8(y, mx_scale_value(code));
+        if (!in) code = 127;
+        // the word: four blocks of eight lanes
+        unsigned word = code << ((lane >> 3 & 3) * 8);
+        word |= __shfl_xor(word, 8);
+        word |= __shfl_xor(word, 16);
+        const int group = i4 >> 5;
+        if ((lane & 31) == 0 && group < groups) scales[(size_t)group * pad + row] = word;
+        if (row == rows - 1 && group < groups && rows + (lane & 31) < pad) scales[(size_t)group * pad + rows + (lane & 31)] = 0x7f7f7f7fu;
+    }
+}
+
+void mx_launch_norm(const float* h, const float* partials, int n_part, size_t part_stride, const float* gain, float eps, int rows, int cols,
+                    float* h_out, void* codes, void* scales, hipStream_t st) {
+    auto run = [&](auto np) {
+        k_mx_norm<decltype(np)::value><<<rows, MX_NORM_T, 0, st>>>(h, partials, part_stride, gain, eps, rows, cols, h_out, (uint8_t*)codes, (uint32_t*)scales);
+    };
+    switch (n_part) {
+        case 0: return run(std::integral_constant<int, 0>{});
+        case 1: return run(std::integral_constant<int, 1>{});
+        case 2: return run(std::integral_constant<int, 2>{});
+        case 3: return run(std::integral_constant<int, 3>{});
+        case 4: return run(std::integral_constant<int, 4>{});
+        case 5: return run(std::integral_constant<int, 5>{});
+        case 6: return run(std::integral_constant<int, 6>{});
+        case 7: return run(std::integral_constant<int, 7>{});
+        default: return run(std::integral_constant<int, 8>{});
+    }
+}

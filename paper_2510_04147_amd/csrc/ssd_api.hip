@@ -34,6 +34,16 @@ static void set_err(ssd_ctx* c, const char* fmt, ...) {
 
 static thread_local std::string g_create_err;
 
+int fail_without_ctx(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    g_create_err = buf;
+    return code;
+}
+
 // ------------------------------------------------------------------ static scratch
 // Device memory of the allocation-free entry point (ssd_k_lm_head_static): one array per GPU the
 // library runs on, held until the process ends.  `scratch` is a host-side stand-in for the symbol;

@@ -230,6 +230,9 @@ struct ssd_ctx {
     std::string err;
 };
 
+// Keeps a failure's detail for ssd_last_error(NULL) of the calling thread and returns `code`: the calls that have no context.
+int fail_without_ctx(int code, const char* fmt, ...);
+
 // ---- launchers implemented in the kernel files (all asynchronous on `st`)
 // T-typed buffers are passed as void* with the dtype flag.
 // What a forward uploads from the pinned staging slot, in words: the header's front, its groups, its nodes (to the same place
