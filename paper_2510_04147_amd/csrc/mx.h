@@ -61,7 +61,16 @@ struct MxArgs {
 void mx_launch_quantize(const void* src, int dtype, int rows, int cols, int format, void* codes, void* scales, void* values, hipStream_t st);
 void mx_launch_norm(const float* h, const float* partials, int n_part, size_t part_stride, const float* gain, float eps, int rows, int cols,
                     float* h_out, void* codes, void* scales, hipStream_t st);
-// The product; fp32 results are *n_part partial sums for the consumer to add by halves, the other results are complete
+// The product; fp32 results are *n_part partial sums for the consumer to add by halves (a.split > 1 yields no other result).  False if a
+// kernel could not be set up.
 bool mx_launch_gemm(const MxArgs& a, int result, int* n_part);
+// the same sums by a wave per 32 x 32 outputs
+void mx_launch_gemm_plain(const MxArgs& a, int result, int* n_part);
+bool mx_gemm_f32(const MxArgs& a, int kind, int* n_part);
+bool mx_gemm_f32_large(const MxArgs& a, int kind, int* n_part);
+bool mx_gemm_bf16(const MxArgs& a, int kind, int* n_part);
+bool mx_gemm_bf16_large(const MxArgs& a, int kind, int* n_part);
+bool mx_gemm_swiglu(const MxArgs& a, int kind, int* n_part);
+bool mx_gemm_swiglu_large(const MxArgs& a, int kind, int* n_part);
 // out (bf16 or fp32, [M, N]) = the sum of the n_part partial sums, by halves
 void mx_launch_join(const float* part, int n_part, size_t part_stride, int result, void* out, size_t n, hipStream_t st);

@@ -1,6 +1,7 @@
 // What the kernels of the microscaled product share.
 #pragma once
 #include "../../include/ssd_mx.h"
+#include "gemm_mfma.h"
 #include "mx.h"
 
 typedef int mx_int8 __attribute__((ext_vector_type(8)));
@@ -61,4 +62,375 @@ __device__ __forceinline__ void mx_store4(bf16_t* p, const float* v, int left, b
 #pragma unroll
         for (int j = 0; j < 4; ++j) if (j < left) p[j] = (bf16_t)u[j];
     }
+}
+
+// ------------------------------------------------------------------------
+// The product's kernel.  Work-group = WN x WM waves, wave (wn, wm) owns TN tiles of 32 weight rows x TM tiles of 32 activation rows and
+// walks every column of the work-group's k-slice: one chain of matrix instructions per output, the same in every shape of this
+// template and in the plain kernel, so a row's bits do not depend on the shape that a call takes.
+//
+// Codes and scales go global -> LDS without passing through registers, in chunks of KC columns: weight rows of KC / 2
+// bytes, activation rows of KC bytes, 16-byte piece s of row r in slot s ^ f(r), so that the 32 rows of a fragment spread over all LDS banks, and
+// per tile and group of 128 columns a line of 32 scale words, into a ring of NST stages.  From the barrier in front of chunk c on, whose
+// stage has landed and with which everyone has read chunk c - 1, chunk c - 1 + NST is loaded into the stage of chunk c - 1.
+//
+// A matrix instruction takes 64 cycles, in which its wave can issue whatever is no matrix instruction: the reads of the next step's fragments
+// and the loads stand between the products one by one (160 rows of the 8B shape's gate/up 29.5 us with all of them in front of the products
+// of a step, 26.1 so; 2304 rows of the 7B class's 285 and 263).  The last step of a chunk runs behind the next barrier.
+//
+// HALVES: the work-group walks two slices and adds their sums (two of four slices: what the consumer adds first).
+// A last chunk that ends inside KC runs as many steps as it has, the other half of a last half step as zeros.
+// ------------------------------------------------------------------------
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
+struct MxShape {
+    static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, G = KC / 128, Q = KC / 64;
+    static constexpr int WROW = KC / 2, XROW = KC, WP = BN * WROW / 1024, XP = BM * XROW / 1024;     // pieces of 1 KB of a chunk
+    // scales: pieces of eight lines, the weights' first; every wave loads equally many pieces of each kind
+    static constexpr int SWP = (BN / 32 * G + 7) / 8, SXP = (BM / 32 * G + 7) / 8, SJ = (SWP + SXP + NW - 1) / NW;
+    static_assert(WP % NW == 0 && XP % NW == 0, "equal shares");
+    static constexpr int WJ = WP / NW, XJ = XP / NW, PER = WJ + XJ + SJ, STAGE = (WP + XP + SJ * NW) * 1024;
+    static_assert(NST >= 2 && PER * (NST - 1) < 64, "ring depth");
+    static constexpr int OUT = 4096;                                         // of a wave: a tile in row order
+    static constexpr int LDS = NST * STAGE > NW * OUT ? NST * STAGE : NW * OUT;
+};
+
+__device__ __forceinline__ int mx_swizzle16(int r, int pieces) { return (r / (16 / pieces)) & (pieces - 1); }
+
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
+__global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks, int m_blocks, int parts) {
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+    constexpr int BN = S::BN, BM = S::BM, G = S::G, Q = S::Q, WROW = S::WROW, XROW = S::XROW, WP = S::WP, SWP = S::SWP, SXP = S::SXP;
+    constexpr int NW = S::NW, STAGE = S::STAGE, XAT = WP * 1024, SAT = XAT + S::XP * 1024;           // a stage: weights, activations, scales
+    constexpr int WJ = S::WJ, XJ = S::XJ, SJ = S::SJ, PER = S::PER;
+    constexpr bool CHANNELS = RESULT == SSD_MX_OUT_SWIGLU;
+    static_assert(!CHANNELS || TN % 2 == 0, "gate and up tiles in pairs");
+    extern __shared__ uint4 smem_u4[];
+    char* const smem = (char*)smem_u4;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave % WN, wm = wave / WN, lm = lane & 31, lh = lane >> 5;
+
+    // Work-groups go to the 8 XCDs round-robin by their id, and every XCD has an L2 of its own: an XCD takes tiles that are neighbours
+    // (the k-slice slowest, then the weights, the rows of one n-block next to each other).
+    int bx, by, bz;
+    {
+        const int total = n_blocks * m_blocks * parts, id = blockIdx.x;
+        const int per = total / 8, more = total % 8, xcd = id & 7;
+        const int t = xcd * per + (xcd < more ? xcd : more) + (id >> 3);
+        by = t % m_blocks;
+        bx = (t / m_blocks) % n_blocks;
+        bz = t / (m_blocks * n_blocks);
+    }
+    const int K = a.K, k_len = mx_slice(K, a.split), spw = HALVES ? 2 : 1;
+    const int k0 = bz * spw * k_len, k1 = min(K, k0 + spw * k_len);
+    const int nchunks = (k1 - k0 + KC - 1) / KC, tail = (k1 - k0) % KC;      // tail: columns of a last chunk that is not whole
+    const int whole = tail ? nchunks - 1 : nchunks;
+    const int boundary = HALVES ? k_len / KC : 0;
+    const int F = a.N / 2, m0 = by * BM;
+    // first weight row of the work-group's tile t; past the end: the last tile (never stored)
+    auto tile_row = [&](int t) SSD_INLINE {
+        if constexpr (CHANNELS) {
+            const int c = min(bx * (BN / 64) + t / 2, F / 32 - 1) * 32;
+            return t % 2 ? F + c : c;
+        } else
+            return min(bx * (BN / 32) + t, (a.N - 1) / 32) * 32;
+    };
+
+    floatx16 acc[TN][TM], tot[HALVES ? TN : 1][HALVES ? TM : 1];
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
+    auto flush = [&]() SSD_INLINE {
+        if constexpr (HALVES)
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int m = 0; m < TM; ++m) {
+                    tot[n][m] = acc[n][m];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
+                }
+    };
+    // Fragments of a step; its scale words are those of a group, two steps: byte 0 or 2, shifted by the lane's half, is the block's.
+    struct Frags { uint4 w[TN], x[TM][2]; unsigned sw[TN], sx[TM]; };
+    const int fw = mx_swizzle16(lm, WROW / 16), fx = mx_swizzle16(lm, XROW / 16), shift = lh * 8;
+    constexpr int CODES = TN + 2 * TM, READS = CODES + TN + TM;              // reads of a step: codes, and scales if it is even
+    auto read1 = [&](auto ec, Frags& f, int slot, int q) SSD_INLINE {        // read e of step q
+        constexpr int e = decltype(ec)::value;
+        const char* w = smem + slot * STAGE;
+        if constexpr (e < TN)
+            f.w[e] = *(const uint4*)(w + (wn * TN + e) * (32 * WROW) + lm * WROW + (((2 * q + lh) ^ fw) << 4));
+        else if constexpr (e < CODES) {
+            constexpr int m = (e - TN) / 2, h = (e - TN) % 2;
+            f.x[m][h] = *(const uint4*)(w + XAT + (wm * TM + m) * (32 * XROW) + lm * XROW + (((4 * q + 2 * h + lh) ^ fx) << 4));
+        } else {
+            const char* r = w + SAT + (q / 2) * 128 + lm * 4;
+            if constexpr (e < CODES + TN) f.sw[e - CODES] = *(const unsigned*)(r + (wn * TN + e - CODES) * (G * 128));
+            else f.sx[e - CODES - TN] = *(const unsigned*)(r + SWP * 1024 + (wm * TM + e - CODES - TN) * (G * 128));
+        }
+    };
+    auto multiply1 = [&](auto jc, auto odd, const Frags& f) SSD_INLINE {
+        constexpr int n = decltype(jc)::value / TM, m = decltype(jc)::value % TM;
+        acc[n][m] = mx_mfma<decltype(odd)::value * 2>(f.w[n], f.x[m][0], f.x[m][1], f.sw[n] >> shift, f.sx[m] >> shift, acc[n][m]);
+    };
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    constexpr std::integral_constant<int, CODES> codes{};
+    constexpr std::integral_constant<int, READS> all{};
+
+    // ---- the walk over the chunks
+    {
+        constexpr int WL = WROW / 16, XL = XROW / 16;                        // lanes to a row
+        const int wrow0 = tile_row(0), urow0 = CHANNELS ? tile_row(1) : wrow0;
+        const uint64_t wbase = (uint64_t)a.w + (size_t)wrow0 * (K / 2) + k0 / 2, up_rows = (uint64_t)(urow0 - wrow0) * (K / 2);
+        const uint64_t xbase = (uint64_t)a.x + (size_t)m0 * K + k0;
+        unsigned off[PER];                                                   // a lane's place from the base
+        uint64_t sbase[SJ];
+        unsigned sstep[SJ];
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) {
+            const int r0 = (wave + NW * j) * (64 / WL), row0 = tile_row(r0 / 32), r = r0 % 32 + lane / WL;
+            const int from = CHANNELS && r0 / 32 % 2 ? urow0 + 0 : wrow0 + 0;
+            off[j] = (unsigned)(min(row0 + r, a.N - 1) - from) * (unsigned)(K / 2) + ((lane % WL) ^ mx_swizzle16(r, WL)) * 16;
+        }
+#pragma unroll
+        for (int j = 0; j < XJ; ++j) {
+            const int r = (wave + NW * j) * (64 / XL) + lane / XL;
+            off[WJ + j] = (unsigned)(min(m0 + r, a.M - 1) - m0) * (unsigned)K + ((lane % XL) ^ mx_swizzle16(r, XL)) * 16;
+        }
+        // line q (tile q / G, group q % G) of the weights' or the activations' scales; past the last: the last again
+        auto scale_line = [&](int j, bool& of_w) SSD_INLINE {
+            const int s = min(wave + NW * j, SWP + SXP - 1);
+            of_w = s < SWP;
+            return min((of_w ? s : s - SWP) * 8 + lane / 8, (of_w ? BN : BM) / 32 * G - 1);
+        };
+#pragma unroll
+        for (int j = 0; j < SJ; ++j) {
+            bool of_w;
+            const int q = scale_line(j, of_w), pad = of_w ? mx_pad_rows(a.N) : mx_pad_rows(a.M);
+            const int row0 = of_w ? tile_row(q / G) : min(m0 / 32 + q / G, (a.M - 1) / 32) * 32;
+            sbase[j] = (of_w ? (uint64_t)a.ws : (uint64_t)a.xs) + (size_t)(k0 >> 7) * pad * 4;
+            sstep[j] = (unsigned)pad * (G * 4);
+            off[WJ + XJ + j] = ((unsigned)(q % G) * pad + row0) * 4u + (lane & 7) * 16;
+        }
+        // load i of chunk `at` into stage `slot`
+        auto issue = [&](auto ic, int slot, int at) SSD_INLINE {
+            constexpr int i = decltype(ic)::value;
+            const unsigned dst = lds0 + slot * STAGE + (wave + NW * i) * 1024;
+            if constexpr (i < WJ) {
+                uint64_t src = wbase + (size_t)at * WROW;
+                if (CHANNELS) src += (wave + NW * i) * (64 / WL) / 32 % 2 ? up_rows + 0 : 0;
+                load_to_lds<NT>(dst, off[i], (const char*)src);
+            } else if constexpr (i < WJ + XJ)
+                load_to_lds<false>(dst, off[i], (const char*)(xbase + (size_t)at * XROW));
+            else
+                load_to_lds<false>(dst, off[i], (const char*)(sbase[i - WJ - XJ] + (size_t)at * sstep[i - WJ - XJ]));
+        };
+        // before the last chunk, if it is not whole, is loaded: what lies past the end of the rows reads something of theirs instead
+        auto shorten = [&]() SSD_INLINE {
+#pragma unroll
+            for (int j = 0; j < WJ; ++j) {
+                const int s = (lane % WL) ^ mx_swizzle16((wave + NW * j) * (64 / WL) % 32 + lane / WL, WL);
+                if (s * 32 >= tail) off[j] -= s * 16;
+            }
+#pragma unroll
+            for (int j = 0; j < XJ; ++j) {
+                const int s = (lane % XL) ^ mx_swizzle16((wave + NW * j) * (64 / XL) + lane / XL, XL);
+                if (s * 16 >= tail) off[WJ + j] -= s * 16;
+            }
+#pragma unroll
+            for (int j = 0; j < SJ; ++j) {
+                bool of_w;
+                const int q = scale_line(j, of_w) % G;
+                if (q * 128 >= tail) off[WJ + XJ + j] -= q * (sstep[j] / G);
+            }
+        };
+        Frags fa, fb;
+        int ahead = NST, slot = 0, free = 0;                                 // chunk to load next; stage of the chunk at hand, free stage
+        // A step: the products of f, between them the reads of the next step's fragments (to `to`, from step nq of the chunk at hand; an odd
+        // one shares f's scale words) and the q-th share of the free stage's loads.
+        auto step = [&](auto qc, auto par, const Frags& f, auto reads, Frags& to, int nq, auto load) SSD_INLINE {
+            constexpr int q = decltype(qc)::value, R = decltype(reads)::value, NM = TN * TM, EARLY = NM > 3 ? NM / 2 : NM;
+            constexpr int L0 = q * PER / Q, L1 = (q + 1) * PER / Q;
+            static_for<0, NM>([&](auto jc) SSD_INLINE {
+                constexpr int j = decltype(jc)::value;
+                __builtin_amdgcn_sched_barrier(0);
+                multiply1(jc, par, f);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (j < EARLY) static_for<j * R / EARLY, (j + 1) * R / EARLY>([&](auto ec) SSD_INLINE { read1(ec, to, slot, nq); });
+                if constexpr (decltype(load)::value) static_for<L0 + j * (L1 - L0) / NM, L0 + (j + 1) * (L1 - L0) / NM>([&](auto ic) SSD_INLINE { issue(ic, free, ahead); });
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (R == CODES) {
+#pragma unroll
+                for (int n = 0; n < TN; ++n) to.sw[n] = f.sw[n];
+#pragma unroll
+                for (int m = 0; m < TM; ++m) to.sx[m] = f.sx[m];
+            }
+        };
+        auto landed = [&](auto bc) SSD_INLINE { wait_and_meet<PER * decltype(bc)::value>(); };        // all but the last bc chunks
+        auto next_stage = [&]() SSD_INLINE {
+            free = slot;
+            slot = slot + 1 == NST ? 0 : slot + 1;
+        };
+        // the steps 0 .. Q - 2 of a chunk whose first fragments are in fa; the last step's end up in fb
+        auto earlier_steps = [&](auto load) SSD_INLINE {
+            step(std::integral_constant<int, 1>{}, even, fa, codes, fb, 1, load);
+            if constexpr (Q == 4) {
+                step(std::integral_constant<int, 2>{}, odd, fb, all, fa, 2, load);
+                step(std::integral_constant<int, 3>{}, even, fa, codes, fb, 3, load);
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < NST; ++u)
+            if (u < nchunks) {
+                if (tail && u == nchunks - 1) shorten();
+                static_for<0, PER>([&](auto ic) SSD_INLINE { issue(ic, u, u); });
+            }
+        if (nchunks >= NST) landed(std::integral_constant<int, NST - 1>{});
+        else landed(std::integral_constant<int, 0>{});
+        if (whole > 0) {
+            static_for<0, READS>([&](auto ec) SSD_INLINE { read1(ec, fa, 0, 0); });
+            earlier_steps(std::false_type{});
+            int c = 1;
+            // from the barrier in front of chunk c on: the last step of the chunk before, whose stage is free, and all but the last of its own.
+            // Without branches, across which the compiler would move the products together.
+            auto period = [&](auto load) SSD_INLINE {
+                constexpr bool LOAD = decltype(load)::value;
+                landed(std::integral_constant<int, LOAD ? NST - 2 : 0>{});
+                if (LOAD && tail && ahead == nchunks - 1) shorten();
+                next_stage();
+                step(std::integral_constant<int, 0>{}, odd, fb, all, fa, 0, load);
+                if (HALVES && c == boundary) flush();
+                earlier_steps(load);
+                if (LOAD) ++ahead;
+                ++c;
+            };
+            const int loading = max(0, min(nchunks - NST, whole - 1)), rest = whole - 1 - loading;
+            for (int i = 0; i < loading; ++i) period(std::true_type{});
+            for (int i = 0; i < rest; ++i) period(std::false_type{});
+            static_for<0, TN * TM>([&](auto jc) SSD_INLINE { multiply1(jc, odd, fb); });
+        }
+        if (tail) {
+            if (whole > 0) {
+                landed(std::integral_constant<int, 0>{});
+                next_stage();
+                if (HALVES && whole == boundary) flush();
+            }
+            for (int q = 0; q * 64 < tail; ++q) {
+                Frags f;
+                static_for<0, READS>([&](auto ec) SSD_INLINE { read1(ec, f, slot, q); });
+                const bool half = q * 64 + 32 >= tail;                       // 32 columns are left: blocks 1 are zeros
+                const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < TN; ++n) {
+                    if (half && lh) f.w[n] = zero;
+                    f.sw[n] = half && lh ? 127u << 8 : f.sw[n] >> (q % 2 * 16);
+                }
+#pragma unroll
+                for (int m = 0; m < TM; ++m) {
+                    if (half) f.x[m][1] = zero;
+                    f.sx[m] = half && lh ? 127u << 8 : f.sx[m] >> (q % 2 * 16);
+                }
+                static_for<0, TN * TM>([&](auto jc) SSD_INLINE { multiply1(jc, even, f); });
+            }
+        }
+    }
+    if constexpr (HALVES) {
+        // one slice alone, where rounding up to chunks leaves the other one empty
+        if (k1 - k0 > k_len)
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[n][m][i] = tot[n][m][i] + acc[n][m][i];
+    }
+
+    // ---- results.  Lane (lm, lh) holds, per tile, weight rows 8 g + 4 lh + j of activation row lm.  They pass through LDS, where
+    // every wave has an area of its own, into row order, so that a store covers whole pieces of rows.
+    __syncthreads();                                                         // the last fragments of the ring have been read
+    char* const area = smem + wave * S::OUT;
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+        const int row0 = m0 + (wm * TM + m) * 32;
+        if constexpr (CHANNELS) {
+            constexpr int PR = TN, LINE = PR * 16 + 16;                      // 16-byte pieces of a row; bytes of its line in LDS
+            static_assert(32 * LINE <= S::OUT, "a wave's area");
+            const int ch0 = (bx * (BN / 64) + wn * TN / 2) * 32, row = row0 + lm;
+            wave_lds_order();                                                // every lane has read what is overwritten next
+#pragma unroll
+            for (int n = 0; n < TN; n += 2) {
+                const int ch = ch0 + n * 16;
+                const unsigned code = mx_store_channels(acc[n][m], acc[n + 1][m], lh, (uint8_t*)area + lm * LINE + n * 16, true);
+                if (lh == 0 && row < mx_pad_rows(a.M) && ch < F) {
+                    uint8_t* word = (uint8_t*)(a.out_s + mx_scale_word(ch >> 7, row, a.M));
+                    word[ch >> 5 & 3] = (uint8_t)(row < a.M ? code : 127);
+                    if (ch + 32 >= F)
+                        for (int b = (ch >> 5 & 3) + 1; b < 4; ++b) word[b] = 127;   // blocks that only fill up the last group
+                }
+            }
+            wave_lds_order();                                                // other lanes wrote what is read next
+#pragma unroll
+            for (int i = 0; i < PR / 2; ++i) {
+                const int r = i * (64 / PR) + lane / PR, at = lane % PR * 16;
+                const uint4 v = *(const uint4*)(area + r * LINE + at);
+                if (row0 + r < a.M && ch0 + at < F) *(uint4*)((uint8_t*)a.out + (size_t)(row0 + r) * F + ch0 + at) = v;
+            }
+        } else {
+            using T = std::conditional_t<RESULT == SSD_MX_OUT_F32, float, bf16_t>;
+            float4* const t = (float4*)area;                                 // 32 lines of 128 bytes, piece s of line r in slot s ^ (r % 8)
+            const bool whole4 = a.N % 4 == 0;
+#pragma unroll
+            for (int n = 0; n < TN; ++n) {
+                wave_lds_order();
+#pragma unroll
+                for (int g = 0; g < 4; ++g) t[lm * 8 + ((g * 2 + lh) ^ (lm & 7))] = make_float4(acc[n][m][4 * g], acc[n][m][4 * g + 1], acc[n][m][4 * g + 2], acc[n][m][4 * g + 3]);
+                wave_lds_order();
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int r = g * 8 + (lane >> 3), col = bx * BN + (wn * TN + n) * 32 + (lane & 7) * 4;
+                    const float4 o = t[r * 8 + ((lane & 7) ^ (r & 7))];
+                    const float v[4] = {o.x, o.y, o.z, o.w};
+                    if (row0 + r < a.M) mx_store4((T*)a.out + (size_t)bz * a.part_stride + (size_t)(row0 + r) * a.N + col, v, a.N - col, whole4);
+                }
+            }
+        }
+    }
+}
+
+// Launches one shape; *n_part = the partial sums it leaves.
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
+bool mx_launch_shape(const MxArgs& a, int* n_part) {
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+    static_assert(S::LDS <= 160 * 1024, "LDS budget");
+    auto kern = k_mx_gemm<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+    static bool attr_done[64];                               // per device
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return false;
+    if (device >= 64 || !attr_done[device]) {
+        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess) return false;
+        if (device < 64) attr_done[device] = true;
+    }
+    const int slices = mx_slices(a.K, a.split), parts = HALVES ? (slices + 1) / 2 : slices;
+    const int n_blocks = (a.N + S::BN - 1) / S::BN, m_blocks = (a.M + S::BM - 1) / S::BM;
+    *n_part = parts;
+    kern<<<dim3((unsigned)(n_blocks * m_blocks * parts)), S::NW * 64, S::LDS, a.st>>>(a, n_blocks, m_blocks, parts);
+    return true;
+}
+
+// Launches shape `kind` if it is one of FIRST .. LAST and yields RESULT (the shapes are spread over translation units, which compile
+// in parallel); false if not.
+template <int RESULT, int FIRST, int LAST>
+bool mx_launch_kind(const MxArgs& a, int kind, int* n_part) {
+#define MX_KIND_CASE(id, wn, wm, tn, tm, kc, nst, nt, halves, results, ...)                                     \
+    if constexpr (id >= FIRST && id <= LAST && ((results) & (RESULT == SSD_MX_OUT_SWIGLU ? 2 : 1)) != 0 &&       \
+                  !(halves && RESULT != SSD_MX_OUT_F32))                                                         \
+        if (kind == id) return mx_launch_shape<wn, wm, tn, tm, kc, nst, RESULT, halves, nt>(a, n_part);
+    MX_KINDS(MX_KIND_CASE)
+#undef MX_KIND_CASE
+    return false;
 }

@@ -98,11 +98,17 @@ void mx_launch_join(const float* part, int n_part, size_t stride, int result, vo
     else k_mx_join<bf16_t><<<grid, 256, 0, st>>>(part, n_part, stride, (bf16_t*)out, n);
 }
 
-bool mx_launch_gemm(const MxArgs& a, int result, int* n_part) {
+void mx_launch_gemm_plain(const MxArgs& a, int result, int* n_part) {
     const dim3 grid(((result == SSD_MX_OUT_SWIGLU ? a.N / 2 : a.N) + 31) / 32, (a.M + 31) / 32);
     *n_part = a.split;
     if (result == SSD_MX_OUT_F32) k_mx_gemm_plain<SSD_MX_OUT_F32><<<grid, 64, 0, a.st>>>(a);
     else if (result == SSD_MX_OUT_BF16) k_mx_gemm_plain<SSD_MX_OUT_BF16><<<grid, 64, 0, a.st>>>(a);
     else k_mx_gemm_plain<SSD_MX_OUT_SWIGLU><<<grid, 64, 0, a.st>>>(a);
-    return true;
+}
+
+bool mx_launch_gemm(const MxArgs& a, int result, int* n_part) {
+    const int kind = mx_choose(a.M, a.N, a.K, a.split, result == SSD_MX_OUT_SWIGLU);
+    if (result == SSD_MX_OUT_F32) return mx_gemm_f32(a, kind, n_part) || mx_gemm_f32_large(a, kind, n_part);
+    if (result == SSD_MX_OUT_BF16) return mx_gemm_bf16(a, kind, n_part) || mx_gemm_bf16_large(a, kind, n_part);
+    return mx_gemm_swiglu(a, kind, n_part) || mx_gemm_swiglu_large(a, kind, n_part);
 }
