@@ -40,43 +40,40 @@ def lib() -> C.CDLL:
     return _lib
 
 
-def _chk(rc):
+# The checks below run in front of every call, whose kernel may take no longer than they do: a device is its index here.
+def _bad(t, what):
+    return ValueError(f"{what} is needed, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+
+
+def _operand(t, index, dtype, shape):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise _bad(t, f"a contiguous {dtype} tensor {tuple(shape)} on GPU {index}")
+    return t.data_ptr()
+
+
+def _matrix(x, index, rows, cols, bits):
+    """Pointers of a microscaled matrix."""
+    codes, scales = x
+    return (_operand(codes, index, torch.float8_e4m3fn, (rows, cols)) if bits == FP8 else _operand(codes, index, torch.uint8, (rows, cols // 2)),
+            _operand(scales, index, torch.float8_e8m0fnu, scale_shape(rows, cols)))
+
+
+def _gpu(t):
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"operands on a GPU are needed, got {t.device}")
+    return index
+
+
+def _call(index, f, *args):
+    """The call on the current stream of the operands' device, which is made the current one for it."""
+    if index == torch.cuda.current_device():
+        rc = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = f(*args, torch._C._cuda_getCurrentRawStream(index))
     if rc < 0:
         raise binding.SsdError(rc, _lib.ssd_strerror(rc).decode(), _lib.ssd_last_error(None).decode())
-
-
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-class _On:
-    """The operands' device made the current one, and its stream.  `tensors`: (tensor or None, its type, its shape)."""
-
-    def __init__(self, *tensors):
-        dev = tensors[0][0].device
-        for t, dtype, shape in tensors:
-            if t is None:
-                continue
-            if not (t.device == dev and dev.type == "cuda"):
-                raise ValueError(f"operands on one GPU are needed, got {t.device} and {dev}")
-            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-                raise ValueError(f"a contiguous {dtype} tensor {tuple(shape)} is needed, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-        self.dev = dev
-
-    def __enter__(self):
-        self.prev = torch.cuda.current_device()
-        if self.prev != self.dev.index:
-            torch.cuda.set_device(self.dev)
-        return torch.cuda.current_stream(self.dev).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.prev != self.dev.index:
-            torch.cuda.set_device(self.prev)
 
 
 def scale_shape(rows, cols):
@@ -89,45 +86,40 @@ def empty(rows, cols, bits, device):
     return codes, torch.empty(scale_shape(rows, cols), dtype=torch.float8_e8m0fnu, device=device)
 
 
-def _form(x, rows, cols, bits):
-    """What _On checks of a microscaled matrix."""
-    _need(isinstance(x, (tuple, list)) and len(x) == 2, "a microscaled matrix is a pair (codes, scales)")
-    return ((x[0], torch.float8_e4m3fn if bits == FP8 else torch.uint8, (rows, cols * bits // 8)),
-            (x[1], torch.float8_e8m0fnu, scale_shape(rows, cols)))
-
-
 def quantize(x, bits, values=None, out=None):
     """x: float32 or bfloat16 [rows, cols], cols a multiple of 32 -> (codes, scales) of `bits` (FP4 or FP8) per value.
     values (as x, may be None) receives the rounded values; out: (codes, scales) to write to."""
-    l = lib()
-    _need(x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16), f"a float32 or bfloat16 matrix is needed, got {x.dtype} {tuple(x.shape)}")
-    rows, cols = x.shape
-    _need(rows > 0 and cols > 0 and cols % 32 == 0, f"columns in blocks of 32 are needed, got {tuple(x.shape)}")
-    _need(bits in (FP4, FP8), f"bits must be 4 or 8, got {bits}")
+    l, index, dtype, shape = lib(), _gpu(x), x.dtype, x.shape
+    if len(shape) != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
+        raise _bad(x, "a float32 or bfloat16 matrix")
+    rows, cols = shape
+    if rows < 1 or cols < 1 or cols % 32:
+        raise _bad(x, "a matrix with columns in blocks of 32")
+    if bits != FP4 and bits != FP8:
+        raise ValueError(f"bits must be 4 or 8, got {bits}")
     if out is None:
         out = empty(rows, cols, bits, x.device)
-    with _On((x, x.dtype, x.shape), (values, x.dtype, x.shape), *_form(out, rows, cols, bits)) as st:
-        _chk(l.ssd_mx_quantize(x.data_ptr(), binding.SSD_F32 if x.dtype == torch.float32 else binding.SSD_BF16, rows, cols, bits,
-                               out[0].data_ptr(), out[1].data_ptr(), _ptr(values), st))
+    _call(index, l.ssd_mx_quantize, _operand(x, index, dtype, shape), binding.SSD_F32 if dtype is torch.float32 else binding.SSD_BF16, rows, cols, bits,
+          *_matrix(out, index, rows, cols, bits), None if values is None else _operand(values, index, dtype, shape))
     return out
 
 
 def norm(h, partials, gain, eps, h_out=None, out=None, keep=True):
     """h + partials (float32 [rows, cols], [n, rows, cols] or None), RMSNorm with `gain` -> (codes, scales), 8 bits.  The sum goes to
     h_out, or to h itself where h_out is None and keep is true."""
-    l = lib()
-    _need(h.dim() == 2 and h.shape[0] > 0 and h.shape[1] > 0 and h.shape[1] % 32 == 0, f"rows in blocks of 32 columns are needed, got {tuple(h.shape)}")
-    rows, cols = h.shape
-    n = 0 if partials is None else partials.shape[0]
-    _need(n == 0 or partials.dim() == 3, "partial sums are [n, rows, cols]")
+    l, index, f32, shape = lib(), _gpu(h), torch.float32, h.shape
+    if len(shape) != 2 or shape[0] < 1 or shape[1] < 1 or shape[1] % 32:
+        raise _bad(h, "a matrix with columns in blocks of 32")
+    rows, cols = shape
+    n, parts = 0, None
+    if partials is not None:
+        n = partials.shape[0] if partials.dim() == 3 else -1
+        parts = _operand(partials, index, f32, (n, rows, cols))
     if out is None:
         out = empty(rows, cols, FP8, h.device)
-    f32 = torch.float32
-    with _On((h, f32, h.shape), (partials if n else None, f32, (n, rows, cols)), (gain, f32, (cols,)), (h_out, f32, h.shape),
-             *_form(out, rows, cols, FP8)) as st:
-        to = h_out if h_out is not None else h if keep else None
-        _chk(l.ssd_mx_norm(h.data_ptr(), _ptr(partials) if n else None, n, gain.data_ptr(), eps, rows, cols, _ptr(to), out[0].data_ptr(),
-                           out[1].data_ptr(), st))
+    at = _operand(h, index, f32, shape)
+    to = _operand(h_out, index, f32, shape) if h_out is not None else at if keep else None
+    _call(index, l.ssd_mx_norm, at, parts, n, _operand(gain, index, f32, (cols,)), eps, rows, cols, to, *_matrix(out, index, rows, cols, FP8))
     return out
 
 
@@ -135,30 +127,37 @@ def linear(x, w, result="bf16", out=None, workspace=None):
     """x (8 bits, [M, K]) times w (4 bits, [N, K]) transposed.  result "bf16" or "fp32": a tensor [M, N]; "swiglu": w holds gate
     rows, then up rows, and the result is silu(gate) * up as (codes, scales) of 8 bits, [M, N / 2].  workspace: a uint8 tensor of at
     least linear_workspace(...) bytes, else one is allocated where the product needs it."""
-    l = lib()
-    _need(result in RESULTS, f"result must be one of {sorted(RESULTS)}, got {result!r}")
-    _need(len(x) == 2 and len(w) == 2 and x[0].dim() == 2 and w[0].dim() == 2, "microscaled matrices are pairs (codes, scales)")
-    M, K = x[0].shape
-    N, kind = w[0].shape[0], RESULTS[result]
-    _need(M > 0 and N > 0 and K > 0 and K % 32 == 0, f"rows in blocks of 32 columns are needed, got {M} x {K} and {N} rows of weights")
-    _need(kind != OUT_SWIGLU or N % 64 == 0, f"gate and up rows in blocks of 32 are needed, got {N}")
-    dev = x[0].device
+    l, kind = lib(), RESULTS.get(result)
+    if kind is None:
+        raise ValueError(f"result must be one of {sorted(RESULTS)}, got {result!r}")
+    codes = x[0]
+    index, shape, N = _gpu(codes), codes.shape, w[0].shape[0]
+    if len(shape) != 2 or shape[0] < 1 or shape[1] < 1 or shape[1] % 32:
+        raise _bad(codes, "a matrix with columns in blocks of 32")
+    if N < 1 or (kind == OUT_SWIGLU and N % 64):
+        raise ValueError(f"rows of weights are needed, gate and up rows in blocks of 32, got {N}")
+    M, K = shape
+    xc, xs = _matrix(x, index, M, K, FP8)
+    wc, ws = _matrix(w, index, N, K, FP4)
     if kind == OUT_SWIGLU:
         if out is None:
-            out = empty(M, N // 2, FP8, dev)
-        to, outs = _form(out, M, N // 2, FP8), (out[0].data_ptr(), out[1].data_ptr())
+            out = empty(M, N // 2, FP8, codes.device)
+        to, to_scales = _matrix(out, index, M, N // 2, FP8)
     else:
         dtype = torch.float32 if kind == OUT_F32 else torch.bfloat16
         if out is None:
-            out = torch.empty(M, N, dtype=dtype, device=dev)
-        to, outs = ((out, dtype, (M, N)),), (out.data_ptr(), None)
-    with _On(*_form(x, M, K, FP8), *_form(w, N, K, FP4), *to) as st:
-        need = l.ssd_mx_linear_workspace(M, N, K, kind)
-        if need and workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _need(workspace is None or (workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == dev), "a contiguous uint8 workspace on the operands' device is needed")
-        _chk(l.ssd_mx_linear(x[0].data_ptr(), x[1].data_ptr(), M, w[0].data_ptr(), w[1].data_ptr(), N, K, kind, *outs, _ptr(workspace),
-                             workspace.numel() if workspace is not None else 0, st))
+            out = torch.empty(M, N, dtype=dtype, device=codes.device)
+        to, to_scales = _operand(out, index, dtype, (M, N)), None
+    at, size = None, 0
+    if workspace is None:
+        size = l.ssd_mx_linear_workspace(M, N, K, kind)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=codes.device)
+            at = workspace.data_ptr()
+    else:
+        size = workspace.numel()
+        at = _operand(workspace, index, torch.uint8, (size,))
+    _call(index, l.ssd_mx_linear, xc, xs, M, wc, ws, N, K, kind, to, to_scales, at, size)
     return out
 
 

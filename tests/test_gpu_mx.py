@@ -225,7 +225,7 @@ def test_refusals(mx):
     w = mx.quantize(torch.zeros(64, 64, device="cuda"), 4)
     bad = [lambda: mx.quantize(x.half(), 8), lambda: mx.quantize(x[:, :40].contiguous(), 8), lambda: mx.quantize(x.t(), 8),
            lambda: mx.quantize(torch.zeros(64, 4, device="cuda").t(), 8), lambda: mx.quantize(x, 6), lambda: mx.quantize(x.cpu(), 8),
-           lambda: mx.quantize(x[:0], 8), lambda: mx.quantize(x, 8, values=x.bfloat16()),
+           lambda: mx.quantize(x[:0], 8), lambda: mx.norm(x, x[None, :2], torch.ones(64, device="cuda"), 1e-5), lambda: mx.quantize(x, 8, values=x.bfloat16()),
            lambda: mx.norm(x, x, torch.ones(64, device="cuda"), 1e-5), lambda: mx.norm(x, None, torch.ones(32, device="cuda"), 1e-5),
            lambda: mx.norm(x.double(), None, torch.ones(64, device="cuda"), 1e-5),
            lambda: mx.linear(f, f, "bf16"), lambda: mx.linear(w, w, "bf16"), lambda: mx.linear(f, w, "int8"), lambda: mx.linear(f, (w[0][:32], w[1]), "bf16"),
