@@ -60,6 +60,7 @@ extern "C" {
 
 #define SSD_F32  0
 #define SSD_BF16 1
+#define SSD_MXFP4 2   /* ssd_config.dtype only: bf16 models whose layer projections ssd_create quantises to 4 bits (ssd_mx.h) */
 
 #define SSD_MAX_BLOCK 64   /* a block's masked set is one 64-bit word; one lane per position */
 #define SSD_MAX_DRAFT 15
@@ -69,7 +70,9 @@ typedef struct ssd_ctx ssd_ctx;   /* opaque */
 typedef struct {
     int n_layers, d_model, n_q_heads, n_kv_heads, head_dim, d_ffn, vocab, mask_id;
                                /* d_model <= 8192, a multiple of 8; head_dim 64 or 128           */
-    int dtype;                 /* SSD_F32 or SSD_BF16: type of weights, KV cache, GEMM operands */
+    int dtype;                 /* SSD_F32 or SSD_BF16: type of weights, KV cache, GEMM operands.  SSD_MXFP4: weights are given in
+                                  bf16 (16-byte aligned; d_model and d_ffn multiples of 32), the layers' projections run on
+                                  4-bit copies of them with 8-bit activations, everything else as SSD_BF16                   */
     float rope_theta, rms_eps;
     int max_seqs;              /* sequence slots in the KV cache                               */
     int max_seq_len;           /* positions per sequence slot (prompt + generation)            */
@@ -123,7 +126,8 @@ size_t ssd_workspace_bytes(const ssd_config* cfg);
 
 /* Create a context.  `workspace` is device memory of at least ssd_workspace_bytes(cfg),
  * 256-byte aligned; `hip_stream` is a hipStream_t (NULL = the default stream).
- * bf16 weights are repacked into the workspace by kernels on `hip_stream`; the call first waits
+ * bf16 weights are repacked into the workspace (SSD_MXFP4: the layers' projections quantised to SSD_MX_FP4, after which the
+ * caller's copies of them are not read again; the LM head repacked) by kernels on `hip_stream`; the call first waits
  * for the device (hipDeviceSynchronize), so weights written on any stream of it are complete.
  * Errors: SSD_EINVAL (null / inconsistent config), SSD_ERANGE (block, draft,
  * d_model or head_dim beyond the supported limits), SSD_ENOMEM, SSD_EHIP. */

@@ -26,6 +26,7 @@ extern "C" {
  * matrix-core kernels read 16 bytes at a time: rows that start elsewhere are copied into the context's workspace first, to an
  * activation buffer that every forward writes anew.)
  * Split-K partial sums are added as the forward's consumers do: the first half of them in split order, the second half, then both.
+ * On an SSD_MXFP4 context SSD_LIN_LM only (x bf16); its projections are what ssd_mx_linear computes (ssd_mx.h).
  * Asynchronous on the context's stream.  Errors: SSD_EINVAL, SSD_ERANGE. */
 int ssd_k_linear(ssd_ctx* ctx, int which, int layer, const void* x, int M, void* out);
 
@@ -55,7 +56,8 @@ int ssd_k_write_cache(ssd_ctx* ctx, int seq, int layer, int pos0, int n, const v
 int ssd_k_attention(ssd_ctx* ctx, int layer, int n_nodes, const ssd_k_node* nodes, const float* qkv, int n_part,
                     int fused, void* out_attn, void* out_q, void* out_k, void* out_v);
 
-/* The residual + RMSNorm step (Section 3.1's f_theta): h (device fp32 [M, d_model], in and out) += the
+/* The residual + RMSNorm step (Section 3.1's f_theta; of an SSD_MXFP4 context the last one, in front of the LM head, the
+ * layers' is ssd_mx_norm; bf16 rows): h (device fp32 [M, d_model], in and out) += the
  * n_part split-K partial sums `partials` (device fp32 [n_part, M, d_model], the first half's sum, then the second's; n_part may be
  * 0), then out (cfg.dtype [M, d_model]) = h / sqrt(mean(h^2) + rms_eps) * gain (device fp32 [d_model]).
  * Asynchronous.  Errors: SSD_EINVAL, SSD_ERANGE. */

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libssd_mi355x.so")
 MEASURE_LIB_PATH = os.path.join(_HERE, "libssd_measure.so")
 
 SSD_MAX_DRAFT = 15
-SSD_F32, SSD_BF16 = 0, 1
+SSD_F32, SSD_BF16, SSD_MXFP4 = 0, 1, 2
 
 EXPORTS = ["ssd_workspace_bytes", "ssd_create", "ssd_destroy", "ssd_reset", "ssd_cached_len", "ssd_prefill_kv",
            "ssd_draft", "ssd_verify_tree", "ssd_generate", "ssd_set_kernel_path", "ssd_set_boundary_fusion", "ssd_set_graphs", "ssd_set_tree_mode", "ssd_set_cross_block",
@@ -134,7 +134,7 @@ def make_config(cfg: dict, max_seqs: int, max_seq_len: int, block: int, max_draf
     c = SsdConfig()
     for n in ("n_layers", "d_model", "n_q_heads", "n_kv_heads", "head_dim", "d_ffn", "vocab", "mask_id"):
         setattr(c, n, int(cfg[n]))
-    c.dtype = SSD_F32 if cfg["dtype"] == "fp32" else SSD_BF16
+    c.dtype = {"fp32": SSD_F32, "mxfp4": SSD_MXFP4}.get(cfg["dtype"], SSD_BF16)
     c.rope_theta, c.rms_eps = float(cfg["rope_theta"]), float(cfg["rms_eps"])
     c.max_seqs, c.max_seq_len, c.block, c.max_draft = max_seqs, max_seq_len, block, max_draft
     c.max_rows = max(max_rows, max_seqs * (max_draft + 1) * block)

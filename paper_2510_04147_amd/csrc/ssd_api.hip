@@ -10,8 +10,10 @@
 #include <cstring>
 #include <new>
 
+#include "mx.h"
 #include "ssd_internal.h"
 #include "../../include/ssd_kernels.h"
+#include "../../include/ssd_mx.h"
 
 #define HIPCHK(ctx, call)                                                                   \
     do {                                                                                    \
@@ -89,7 +91,12 @@ static int check_config(const ssd_config* cfg, std::string* why) {
         cfg->vocab < 2 || cfg->max_seqs < 1 || cfg->max_seq_len < 1 || cfg->block < 1 || cfg->max_draft < 0 ||
         cfg->max_rows < 1)
         return bad(SSD_EINVAL, "non-positive dimension");
-    if (cfg->dtype != SSD_F32 && cfg->dtype != SSD_BF16) return bad(SSD_EINVAL, "dtype must be SSD_F32 or SSD_BF16");
+    if (cfg->dtype != SSD_F32 && cfg->dtype != SSD_BF16 && cfg->dtype != SSD_MXFP4) return bad(SSD_EINVAL, "dtype must be SSD_F32, SSD_BF16 or SSD_MXFP4");
+    if (cfg->dtype == SSD_MXFP4 && (cfg->d_model % 32 || cfg->d_ffn % 32)) return bad(SSD_EINVAL, "SSD_MXFP4 needs d_model and d_ffn in multiples of 32");
+    if (cfg->dtype == SSD_MXFP4 && (2ll * cfg->d_ffn > SSD_MX_MAX_ROWS || cfg->max_rows > SSD_MX_MAX_ROWS ||
+                                    ((long long)cfg->n_q_heads + 2ll * cfg->n_kv_heads) * cfg->head_dim > SSD_MX_MAX_ROWS ||
+                                    (long long)cfg->max_rows * std::max(2ll * cfg->d_ffn, ((long long)cfg->n_q_heads + 2ll * cfg->n_kv_heads) * cfg->head_dim) > SSD_MX_MAX_OUT))
+        return bad(SSD_ERANGE, "SSD_MXFP4: a projection beyond the products' sizes");
     if (cfg->n_q_heads % cfg->n_kv_heads) return bad(SSD_EINVAL, "n_q_heads must be a multiple of n_kv_heads");
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return bad(SSD_ERANGE, "head_dim must be 64 or 128");
     if (cfg->d_model % 8 || cfg->d_ffn % 8) return bad(SSD_EINVAL, "d_model and d_ffn must be multiples of 8");
@@ -107,7 +114,9 @@ static int check_config(const ssd_config* cfg, std::string* why) {
 static Dims dims_of(const ssd_config* c) {
     Dims d;
     d.L = c->n_layers; d.d = c->d_model; d.Hq = c->n_q_heads; d.Hkv = c->n_kv_heads; d.dh = c->head_dim;
-    d.F = c->d_ffn; d.V = c->vocab; d.mask_id = c->mask_id; d.dtype = c->dtype; d.eps = c->rms_eps;
+    d.F = c->d_ffn; d.V = c->vocab; d.mask_id = c->mask_id; d.eps = c->rms_eps;
+    d.mx = c->dtype == SSD_MXFP4;
+    d.dtype = d.mx ? SSD_BF16 : c->dtype;
     d.max_seqs = c->max_seqs; d.max_seq_len = c->max_seq_len; d.block = c->block; d.max_draft = c->max_draft;
     d.max_rows = c->max_rows;
     return d;
@@ -122,7 +131,17 @@ static bool packable(const Dims& d, size_t N, size_t K) { return d.dtype == SSD_
 static size_t packed_bytes(const Dims& d) {
     if (d.dtype != SSD_BF16) return 0;
     auto sz = [&](size_t N, size_t K) { return packable(d, N, K) ? ((N * K * 2 + 255) & ~(size_t)255) : 0; };
-    return (sz(d.nqkv(), d.d) + sz(d.d, d.nq()) + sz(2 * (size_t)d.F, d.d) + sz(d.d, d.F)) * d.L + sz(d.V, d.d);
+    return (d.mx ? 0 : (sz(d.nqkv(), d.d) + sz(d.d, d.nq()) + sz(2 * (size_t)d.F, d.d) + sz(d.d, d.F)) * d.L) + sz(d.V, d.d);
+}
+
+// A microscaled matrix of `bits` per value in the workspace: codes, then scales, both on 256-byte boundaries.
+static size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+static size_t mx_code_bytes(size_t rows, size_t cols, int bits) { return align256(rows * cols * bits / 8); }
+static size_t mx_scales_bytes(size_t rows, size_t cols) { return align256((size_t)mx_groups((int)cols) * mx_pad_rows((int)rows) * 4); }
+static size_t mx_weight_bytes(const Dims& d) {
+    if (!d.mx) return 0;
+    auto sz = [&](size_t N, size_t K) { return mx_code_bytes(N, K, 4) + mx_scales_bytes(N, K); };
+    return (sz(d.nqkv(), d.d) + sz(d.d, d.nq()) + sz(2 * (size_t)d.F, d.d) + sz(d.d, d.F)) * d.L;
 }
 
 // Walks the workspace layout; with base == nullptr it only measures.
@@ -143,10 +162,18 @@ static size_t carve(const Dims& d, char* base, Buffers* b) {
     t.kown = take((size_t)d.nkv() * d.vt_rows() * e);
     t.vown = take((size_t)d.nkv() * d.vt_rows() * e);
     t.attn = take(R * d.nq() * e);
-    t.act = take(R * d.F * e);
+    t.act = take(d.mx ? 0 : R * d.F * e);
     const size_t pc = d.nqkv() > d.d ? d.nqkv() : d.d;
     t.part = (float*)take((size_t)SSD_MAX_SPLIT * R * pc * 4);
     t.packed = take(packed_bytes(d));
+    t.mx_weights = take(mx_weight_bytes(d));
+    auto mx_rows = [&](size_t cols, void*& codes, void*& scales) {
+        codes = take(d.mx ? mx_code_bytes(R, cols, 8) : 0);
+        scales = take(d.mx ? mx_scales_bytes(R, cols) : 0);
+    };
+    mx_rows(d.d, t.mx_xn, t.mx_xn_s);
+    mx_rows(d.nq(), t.mx_attn, t.mx_attn_s);
+    mx_rows(d.F, t.mx_act, t.mx_act_s);
     t.lm_part = (float*)take(R * (size_t)tiles * 3 * 4);
     t.row_max = (float*)take(R * 4);
     t.row_arg = (int*)take(R * 4);
@@ -194,6 +221,10 @@ extern "C" __attribute__((visibility("default"))) int ssd_create(const ssd_confi
             g_create_err = "null per-layer weight pointer";
             return SSD_EINVAL;
         }
+    if (d.mx)
+        for (int l = 0; l < d.L; ++l)
+            for (const void* p : {w->wqkv[l], w->wo[l], w->wgu[l], w->wdown[l]})
+                if ((uintptr_t)p & 15) { g_create_err = "SSD_MXFP4: a projection's weights start off a 16-byte boundary"; return SSD_EINVAL; }
     // The repack kernels below read the weights on `hip_stream`; whatever wrote them, on any stream
     // of this device, has to be complete first.  Creation is a one-time set-up call: wait for the device.
     {
@@ -222,7 +253,7 @@ extern "C" __attribute__((visibility("default"))) int ssd_create(const ssd_confi
     {
         char* pk = (char*)c->b.packed;
         auto mk = [&](const void* raw, int N, int K, int gate_rows = 0) {
-            Wt t{raw, nullptr, N, K};
+            Wt t{raw, nullptr, N, K, nullptr, nullptr};
             if (packable(d, N, K)) {
                 t.packed = pk;
                 launch_pack_weights(raw, pk, N, K, gate_rows, c->stream);
@@ -230,8 +261,18 @@ extern "C" __attribute__((visibility("default"))) int ssd_create(const ssd_confi
             }
             return t;
         };
+        char* mp = (char*)c->b.mx_weights;
+        auto mk_mx = [&](const void* raw, int N, int K) {
+            Wt t{raw, nullptr, N, K, mp, mp + mx_code_bytes(N, K, 4)};
+            mx_launch_quantize(raw, SSD_BF16, N, K, SSD_MX_FP4, mp, (void*)t.scales, nullptr, c->stream);
+            mp += mx_code_bytes(N, K, 4) + mx_scales_bytes(N, K);
+            return t;
+        };
         c->lw.resize(d.L);
-        for (int l = 0; l < d.L; ++l)
+        for (int l = 0; l < d.L && d.mx; ++l)
+            c->lw[l] = LayerW{mk_mx(w->wqkv[l], d.nqkv(), d.d), mk_mx(w->wo[l], d.d, d.nq()), mk_mx(w->wgu[l], 2 * d.F, d.d),
+                              mk_mx(w->wdown[l], d.d, d.F), w->norm1[l], w->norm2[l]};
+        for (int l = 0; l < d.L && !d.mx; ++l)
             c->lw[l] = LayerW{mk(w->wqkv[l], d.nqkv(), d.d), mk(w->wo[l], d.d, d.nq()), mk(w->wgu[l], 2 * d.F, d.d, d.F),
                               mk(w->wdown[l], d.d, d.F), w->norm1[l], w->norm2[l]};
         c->lm_head = mk(w->lm_head, d.V, d.d);
@@ -461,6 +502,26 @@ static void gemm(ssd_ctx* c, int cls, int epi, const void* X, const Wt& W, void*
     launch_gemm_plain(c, epi, X, W.raw, out, M, N, W.K, c->stream);
 }
 
+// SSD_MXFP4: out = X W^T of microscaled rows and a layer's projection; SSD_MX_OUT_F32 writes *n_split partial sums as gemm() does,
+// SSD_MX_OUT_SWIGLU the activated channels, microscaled.
+static void gemm_mx(ssd_ctx* c, int result, const void* x, const void* xs, const Wt& W, void* out, void* out_scales, int M, int* n_split) {
+    MxArgs a;
+    a.x = (const uint8_t*)x; a.xs = (const uint32_t*)xs;
+    a.w = (const uint8_t*)W.codes; a.ws = (const uint32_t*)W.scales;
+    a.out = out; a.out_s = (uint32_t*)out_scales;
+    a.part_stride = (size_t)c->dm.max_rows * c->part_cols;
+    a.M = M; a.N = W.N; a.K = W.K; a.split = mx_slices(W.K, mx_split(W.N, W.K, result == SSD_MX_OUT_SWIGLU));
+    a.st = c->stream;
+    if (c->kernel_path >= 1 && mx_launch_gemm(a, result, n_split)) return;
+    mx_launch_gemm_plain(a, result, n_split);
+}
+
+// A layer's norm: partial sums into the residual stream, its rows normed in the type of the projections' operands.
+static void layer_norm(ssd_ctx* c, int M, const float* gain, int n_part) {
+    if (!c->dm.mx) return launch_norm(c, M, gain, n_part, c->stream);
+    mx_launch_norm(c->b.h, c->b.part, n_part, (size_t)c->dm.max_rows * c->part_cols, gain, c->dm.eps, M, c->dm.d, c->b.h, c->b.mx_xn, c->b.mx_xn_s, c->stream);
+}
+
 // Brings a forward's descriptor, its raw tokens and the block states to upload to the device through
 // the pinned staging ring (asynchronous on the context's stream).
 static int stage_forward(ssd_ctx* c, const FwdHeader& hd, const int32_t* raw, int n_raw, const Upload* ups, int n_ups,
@@ -557,12 +618,14 @@ static int run_forward(ssd_ctx* c, const FwdHeader& hd, const int32_t* raw, int 
             ProfScope ps(c, KC_ROWS);
             launch_rows(c, M, hd.n_nodes, c->lw[0].norm1, st);
         }
+        const bool mx = d.mx;
         int n_part = 0, ns = 1;
         for (int l = 0; l < d.L; ++l) {
             const LayerW& w = c->lw[l];
-            if (l > 0) { ProfScope ps(c, KC_NORM); launch_norm(c, M, w.norm1, n_part, st); }
+            if (l > 0 || mx) { ProfScope ps(c, KC_NORM); layer_norm(c, M, w.norm1, n_part); }
             n_part = 0;
-            gemm(c, KC_GEMM_QKV, EPI_F32, c->b.xn, w.wqkv, c->b.part, M, &ns);
+            if (mx) { ProfScope ps(c, KC_GEMM_QKV); gemm_mx(c, SSD_MX_OUT_F32, c->b.mx_xn, c->b.mx_xn_s, w.wqkv, c->b.part, nullptr, M, &ns); }
+            else gemm(c, KC_GEMM_QKV, EPI_F32, c->b.xn, w.wqkv, c->b.part, M, &ns);
             // blocks of at most 32 rows: the attention kernel sums the partial sums and applies the
             // rotary embedding itself; a pure KV pass needs only the last layer's K and V, not its attention
             const bool last_kv_only = l == d.L - 1 && ML == 0;
@@ -582,10 +645,21 @@ static int run_forward(ssd_ctx* c, const FwdHeader& hd, const int32_t* raw, int 
                       launch_attn_mfma(c, nodes, nodes_per_seq, blen, l, fused ? ns : -1, any_suffix, st)))
                     launch_attn_plain(c, R, l, st);
             }
-            gemm(c, KC_GEMM_O, EPI_F32, c->b.attn, w.wo, c->b.part, R, &ns);
-            { ProfScope ps(c, KC_NORM); launch_norm(c, R, w.norm2, ns, st); }
-            gemm(c, KC_GEMM_GU, EPI_SWIGLU, c->b.xn, w.wgu, c->b.act, R, &ns);
-            gemm(c, KC_GEMM_DOWN, EPI_F32, c->b.act, w.wdown, c->b.part, R, &ns);
+            if (mx) {
+                ProfScope ps(c, KC_GEMM_O);                  // with its operand's quantisation
+                mx_launch_quantize(c->b.attn, SSD_BF16, R, d.nq(), SSD_MX_FP8, c->b.mx_attn, c->b.mx_attn_s, nullptr, st);
+                gemm_mx(c, SSD_MX_OUT_F32, c->b.mx_attn, c->b.mx_attn_s, w.wo, c->b.part, nullptr, R, &ns);
+            } else
+                gemm(c, KC_GEMM_O, EPI_F32, c->b.attn, w.wo, c->b.part, R, &ns);
+            { ProfScope ps(c, KC_NORM); layer_norm(c, R, w.norm2, ns); }
+            if (mx) {
+                { ProfScope ps(c, KC_GEMM_GU); gemm_mx(c, SSD_MX_OUT_SWIGLU, c->b.mx_xn, c->b.mx_xn_s, w.wgu, c->b.mx_act, c->b.mx_act_s, R, &ns); }
+                ProfScope ps(c, KC_GEMM_DOWN);
+                gemm_mx(c, SSD_MX_OUT_F32, c->b.mx_act, c->b.mx_act_s, w.wdown, c->b.part, nullptr, R, &ns);
+            } else {
+                gemm(c, KC_GEMM_GU, EPI_SWIGLU, c->b.xn, w.wgu, c->b.act, R, &ns);
+                gemm(c, KC_GEMM_DOWN, EPI_F32, c->b.act, w.wdown, c->b.part, R, &ns);
+            }
             n_part = ns;
         }
         if (ML > 0) {
@@ -1405,6 +1479,7 @@ extern "C" __attribute__((visibility("default"))) int ssd_k_linear(ssd_ctx* c, i
     if (!x || !out || M < 1) { set_err(c, "k_linear: null pointer or M < 1"); return SSD_EINVAL; }
     if (M > d.max_rows) { set_err(c, "k_linear: M exceeds max_rows"); return SSD_ERANGE; }
     if (which != SSD_LIN_LM && (layer < 0 || layer >= d.L)) { set_err(c, "k_linear: layer out of range"); return SSD_ERANGE; }
+    if (which != SSD_LIN_LM && d.mx) { set_err(c, "k_linear: the projections of an SSD_MXFP4 context are microscaled (ssd_mx_linear)"); return SSD_EINVAL; }
     int ns = 1;
     switch (which) {
         case SSD_LIN_QKV:

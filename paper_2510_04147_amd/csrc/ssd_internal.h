@@ -90,6 +90,7 @@ enum KClass : int {
 
 struct Dims {
     int L, d, Hq, Hkv, dh, F, V, mask_id, dtype;
+    bool mx;               // SSD_MXFP4: the layers' projections are microscaled; dtype, that of everything else, is SSD_BF16
     float eps;
     int max_seqs, max_seq_len, block, max_draft, max_rows;
     int nq() const { return Hq * dh; }
@@ -143,6 +144,9 @@ struct Buffers {
     float* part;         // [SSD_MAX_SPLIT, max_rows, max(d, nqkv)] fp32 split-K partial sums of the
                          // QKV, O and down projections (summed by the consumer: the first half of them in order, the second half, then both)
     void* packed;        // fragment-order copies of the weights (bf16 models)
+    void* mx_weights;    // SSD_MXFP4: codes and scales of the layers' projections
+    void *mx_xn, *mx_attn, *mx_act;        // SSD_MXFP4: codes [max_rows, ..] of normed rows, attention output, activated channels
+    void *mx_xn_s, *mx_attn_s, *mx_act_s;  // and their scales
     float* lm_part;      // [max_rows, n_vtiles, 3] (max, arg as float bits, sumexp)
     float* row_max;      // [max_rows]
     int* row_arg;        // [max_rows]
@@ -170,6 +174,7 @@ struct Wt {
     const void* raw;
     const void* packed;
     int N, K;
+    const void *codes, *scales;    // SSD_MXFP4, the layers' projections: 4-bit codes and scales instead
 };
 
 struct LayerW {

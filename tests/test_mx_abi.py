@@ -77,3 +77,29 @@ def test_linear_refusals(lib, change, code, what):
     a.update(change)
     assert lib.ssd_mx_linear(*a.values(), None) == code
     assert what in lib.ssd_last_error(None).decode()
+
+
+def test_contexts(lib):
+    """SSD_MXFP4 in a context's configuration: accepted where the projections have whole blocks, and smaller than bf16."""
+    import ctypes
+    from paper_2510_04147_amd import binding, synth
+    size = lambda c: lib.ssd_workspace_bytes(ctypes.byref(c))  # noqa: E731
+    bf16 = binding.make_config(synth.model_config("8b"), 1, 512, 32, 4)
+    mxfp4 = binding.make_config(synth.model_config("8b", dtype="mxfp4"), 1, 512, 32, 4)
+    assert mxfp4.dtype == binding.SSD_MXFP4 == 2
+    L, d, F = 32, 4096, 12288
+    weights = L * (3 * d * d + d * d + 3 * F * d)
+    assert 0 < size(mxfp4) < size(bf16) - 2 * weights + weights * 17 // 32 + (64 << 20)
+    for field, value in (("d_model", 264), ("d_ffn", 12304), ("d_ffn", 1 << 20), ("max_rows", 1 << 21), ("max_rows", 1 << 20)):
+        bad = binding.make_config(synth.model_config("8b", dtype="mxfp4"), 1, 512, 32, 4)
+        setattr(bad, field, value)
+        assert size(bad) == 0, (field, value)
+    w = binding.SsdWeights()
+    # a projection off a 16-byte boundary is refused before the device is touched
+    one = (ctypes.c_void_p * 32)(*[1 << 20] * 32)
+    odd = (ctypes.c_void_p * 32)(*[(1 << 20) + 2] * 32)
+    p = lambda a: ctypes.cast(a, ctypes.POINTER(ctypes.c_void_p))  # noqa: E731
+    w = binding.SsdWeights(1 << 20, 1 << 20, 1 << 20, p(one), p(odd), p(one), p(one), p(one), p(one))
+    h = ctypes.c_void_p()
+    assert lib.ssd_create(ctypes.byref(mxfp4), ctypes.byref(w), ctypes.c_void_p(256), 1 << 60, None, ctypes.byref(h)) == -1
+    assert b"16-byte" in lib.ssd_last_error(None)
