@@ -24,6 +24,7 @@
 //     a 1-node and an (N+1)-node forward.
 // Forwards with more rows take k_gemm_rows (gemm_rows.h), which computes the same sums in the same order.
 #include "gemm_mfma.h"
+#include "mx.h"
 
 // ------------------------------------------------------------------------
 // One-time weight repack: W[N][K] row-major -> fragment order.
@@ -130,7 +131,7 @@ __device__ __forceinline__ float merge2(float a, float ca, float b, float cb) { 
 // a CU (both times: attn_two_per_cu).  The eight waves, which have the CU to themselves, put all strands' results there in one trip
 // (pairs first, in a trip of their own / this, us: 32 rows at prefix 384, 32 heads 10.8 / 10.5, two nodes 11.3 / 10.7, 193-row prompt of
 // 24 heads 9.7 / 9.2).
-template <int DH, bool FUSED, bool SUFFIX, bool SHARED>
+template <int DH, bool FUSED, bool SUFFIX, bool SHARED, bool MX>
 __global__ __launch_bounds__(SHARED ? 256 : 512, 2) void k_attn_mfma(const FwdHeader* __restrict__ fw,
                                                                const bf16_t* __restrict__ q,
                                                                const bf16_t* __restrict__ kown,
@@ -141,7 +142,8 @@ __global__ __launch_bounds__(SHARED ? 256 : 512, 2) void k_attn_mfma(const FwdHe
                                                                int max_seqs, int seq_stride, int vt_rows, float scale,
                                                                const float* __restrict__ part, int n_part,
                                                                size_t part_stride, const float* __restrict__ cosT,
-                                                               const float* __restrict__ sinT, int nodes_per_seq) {
+                                                               const float* __restrict__ sinT, int nodes_per_seq, int rows,
+                                                               uint8_t* __restrict__ codes, uint32_t* __restrict__ scales) {
     constexpr int KST = DH / 16, DT = DH / 32;
     constexpr int WAVES = SHARED ? 4 : 8, T = WAVES * 64;
     constexpr int NE = DT * 16;                                      // O^T values per lane
@@ -470,7 +472,39 @@ __global__ __launch_bounds__(SHARED ? 256 : 512, 2) void k_attn_mfma(const FwdHe
         for (int w = 0; w < 4; ++w) acc = __fmaf_rn(pair(w, wave * EPW + e), cw[w], acc);
         o[e] = acc * inv;
     }
-    if (qvalid) {
+    if constexpr (MX) {
+        // bf16 as without MX, then 8 bits and a scale for every block of 32 head channels.  The merge spreads a block over 16 / EPW
+        // waves: their maxima meet where the query tile lay.  A kernel of its own for this costs 4 us a layer.
+        constexpr int PER_BLOCK = 16 / EPW;
+        unsigned(*const tops)[32] = (unsigned(*)[32])&qs[0][0];
+        unsigned top = 0;
+#pragma unroll
+        for (int e = 0; e < EPW; ++e) {
+            o[e] = __uint_as_float((uint32_t)f2bf_m(o[e]) << 16);
+            const unsigned mag = __float_as_uint(o[e]) & 0x7fffffffu;
+            top = mag > top ? mag : top;
+        }
+        const unsigned other = other_half(top, lh);
+        top = other > top ? other : top;
+        if (lh == 0) tops[wave][lm] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < PER_BLOCK; ++w) {
+            const unsigned of = tops[wave / PER_BLOCK * PER_BLOCK + w][lm];
+            top = of > top ? of : top;
+        }
+        const unsigned code = mx_scale_code<8>(top);
+        const int c0 = head * DH + (wave / PER_BLOCK) * 32;          // the block's first channel
+        if (qvalid) {
+#pragma unroll
+            for (int g4 = 0; g4 < EPW / 4; ++g4) {
+                const int g = ((wave * EPW + g4 * 4) & 15) >> 2;
+                *(uint32_t*)(codes + (size_t)qrow * nq + c0 + g * 8 + lh * 4) = code == 255 ? 0u : mx_pack8(o + g4 * 4, mx_scale_value(code));
+            }
+            if (wave % PER_BLOCK == 0 && lh == 0)
+                ((uint8_t*)(scales + mx_scale_word(c0 >> 7, qrow, rows)))[c0 >> 5 & 3] = (uint8_t)code;
+        }
+    } else if (qvalid) {
         bf16_t* op = out + (size_t)qrow * nq + head * DH;
 #pragma unroll
         for (int g4 = 0; g4 < EPW / 4; ++g4) {
@@ -490,7 +524,7 @@ bool attn_mfma_can_fuse_rope(const ssd_ctx* c, int max_blen) {
 }
 
 bool launch_attn_mfma(const ssd_ctx* c, int n_nodes, int nodes_per_seq, int max_blen, int layer, int n_part, bool suffix,
-                      hipStream_t st) {
+                      hipStream_t st, int mx_rows) {
     if (nodes_per_seq <= 0 || n_nodes % nodes_per_seq) nodes_per_seq = 0;
     const Dims& d = c->dm;
     dim3 grid(n_nodes * d.Hq, (max_blen + 31) / 32);
@@ -499,11 +533,16 @@ bool launch_attn_mfma(const ssd_ctx* c, int n_nodes, int nodes_per_seq, int max_
 #define SSD_ATTN_ARGS                                                                                                  \
     c->b.fwd, (const bf16_t*)c->b.q, (const bf16_t*)c->b.kown, (const bf16_t*)c->b.vown, (const bf16_t*)c->b.kcache, \
         (const bf16_t*)c->b.vcache, (bf16_t*)c->b.attn, d.Hq, d.Hkv, layer, d.max_seqs, d.seq_stride(), d.vt_rows(), scale, \
-        c->b.part, n_part, ps, c->b.rope_cos, c->b.rope_sin, nodes_per_seq
+        c->b.part, n_part, ps, c->b.rope_cos, c->b.rope_sin, nodes_per_seq, mx_rows, (uint8_t*)c->b.mx_attn, (uint32_t*)c->b.mx_attn_s
+#define SSD_ATTN_RUN_MX(DH_, FUSED_, SUFFIX_, MX_)                                                                      \
+    do {                                                                                                               \
+        if (shared) k_attn_mfma<DH_, FUSED_, SUFFIX_, true, MX_><<<grid, 256, 0, st>>>(SSD_ATTN_ARGS);                 \
+        else k_attn_mfma<DH_, FUSED_, SUFFIX_, false, MX_><<<grid, 512, 0, st>>>(SSD_ATTN_ARGS);                       \
+    } while (0)
 #define SSD_ATTN_RUN(DH_, FUSED_, SUFFIX_)                                                                              \
     do {                                                                                                               \
-        if (shared) k_attn_mfma<DH_, FUSED_, SUFFIX_, true><<<grid, 256, 0, st>>>(SSD_ATTN_ARGS);                      \
-        else k_attn_mfma<DH_, FUSED_, SUFFIX_, false><<<grid, 512, 0, st>>>(SSD_ATTN_ARGS);                            \
+        if (mx_rows > 0) SSD_ATTN_RUN_MX(DH_, FUSED_, SUFFIX_, true);                                                  \
+        else SSD_ATTN_RUN_MX(DH_, FUSED_, SUFFIX_, false);                                                             \
     } while (0)
 #define SSD_ATTN_LAUNCH(DH_, FUSED_)                                                                                   \
     do {                                                                                                               \
@@ -522,6 +561,7 @@ bool launch_attn_mfma(const ssd_ctx* c, int n_nodes, int nodes_per_seq, int max_
         return false;
 #undef SSD_ATTN_LAUNCH
 #undef SSD_ATTN_RUN
+#undef SSD_ATTN_RUN_MX
 #undef SSD_ATTN_ARGS
     return true;
 }

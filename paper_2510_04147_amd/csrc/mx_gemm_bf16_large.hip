@@ -1,4 +1,4 @@
 // Shapes of the microscaled product's kernel (mx_rules.h).
 #include "mx_gemm.h"
 
-bool mx_gemm_bf16_large(const MxArgs& a, int kind, int* n_part) { return mx_launch_kind<SSD_MX_OUT_BF16, 7, 18>(a, kind, n_part); }
+bool mx_gemm_bf16_large(const MxArgs& a, int kind, int* n_part) { return mx_launch_kind<SSD_MX_OUT_BF16, 6, 17>(a, kind, n_part); }

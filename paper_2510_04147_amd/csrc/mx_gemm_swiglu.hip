@@ -1,4 +1,4 @@
 // Shapes of the microscaled product's kernel (mx_rules.h).
 #include "mx_gemm.h"
 
-bool mx_gemm_swiglu(const MxArgs& a, int kind, int* n_part) { return mx_launch_kind<SSD_MX_OUT_SWIGLU, 6, 16>(a, kind, n_part); }
+bool mx_gemm_swiglu(const MxArgs& a, int kind, int* n_part) { return mx_launch_kind<SSD_MX_OUT_SWIGLU, 5, 12>(a, kind, n_part); }

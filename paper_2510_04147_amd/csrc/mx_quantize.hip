@@ -29,7 +29,7 @@ __device__ __forceinline__ unsigned mx_dpp(unsigned v) { return (unsigned)__buil
 __device__ __forceinline__ unsigned mx_max(unsigned a, unsigned b) { return a > b ? a : b; }
 
 // Quantisation.  A work-group of four waves takes 32 rows x 512 columns: a wave reads 512 columns of a row in one go, eight values
-// to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has its eight rows' loads in flight together.
+// to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has the loads of its rows, every fourth, in flight together.
 // The tile's scale words meet in LDS and leave as whole lines.  Reads every value once: bound by memory.
 template <typename T, int BITS, bool VALUES>
 __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, int rows, int cols, uint8_t* __restrict__ codes,
@@ -41,14 +41,18 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
     float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int row = row0 + wave * 8 + i;
+        const int row = row0 + i * 4 + wave;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
         if (in && row < rows) mx_load8(src + (size_t)row * cols + col, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int row = row0 + wave * 8 + i;
+        const int row = row0 + i * 4 + wave;
+        if (row >= rows) {                                   // the wave's: what only fills up
+            if ((lane & 15) == 0) words[lane >> 4][i * 4 + wave] = 0x7f7f7f7fu;
+            continue;
+        }
         unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = mx_max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
         if (code == 255)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-        if (in && row < rows) {
+        if (in) {
             const size_t at = (size_t)row * cols + col;
             if constexpr (BITS == 4) {
                 const unsigned o = mx_pack4(v[i], scale);
@@ -90,12 +94,12 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
                 }
             }
         }
-        if (!in || row >= rows) code = 127;                  // what only fills up
+        if (!in) code = 127;                                 // what only fills up
         // the word: four blocks of four lanes
         unsigned word = code << ((lane >> 2 & 3) * 8);
         word |= mx_dpp<0x141>(word);
         word |= mx_dpp<0x140>(word);
-        if ((lane & 15) == 0) words[lane >> 4][wave * 8 + i] = word;
+        if ((lane & 15) == 0) words[lane >> 4][i * 4 + wave] = word;
     }
     __syncthreads();
     const int group = blockIdx.y * 4 + (threadIdx.x >> 5);
@@ -116,11 +120,26 @@ void mx_launch_quantize(const void* src, int dtype, int rows, int cols, int form
     else typed(bf16_t(0));
 }
 
+// The sum of the wave's 64 values, in every lane, without trips through LDS.
+__device__ __forceinline__ double mx_wave_sum(double v) {
+    auto both = [](double a, unsigned lo, unsigned hi) { return a + __hiloint2double((int)hi, (int)lo); };
+    auto lo = [](double a) { return (unsigned)__double2loint(a); };
+    auto hi = [](double a) { return (unsigned)__double2hiint(a); };
+    v = both(v, mx_dpp<0xB1>(lo(v)), mx_dpp<0xB1>(hi(v)));
+    v = both(v, mx_dpp<0x4E>(lo(v)), mx_dpp<0x4E>(hi(v)));
+    v = both(v, mx_dpp<0x141>(lo(v)), mx_dpp<0x141>(hi(v)));
+    v = both(v, mx_dpp<0x140>(lo(v)), mx_dpp<0x140>(hi(v)));
+    auto l = __builtin_amdgcn_permlane16_swap(lo(v), lo(v), false, false), h = __builtin_amdgcn_permlane16_swap(hi(v), hi(v), false, false);
+    v = __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+    l = __builtin_amdgcn_permlane32_swap(lo(v), lo(v), false, false);
+    h = __builtin_amdgcn_permlane32_swap(hi(v), hi(v), false, false);
+    return __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+}
+
 // RMSNorm behind the residual's addition, output in 8 bits.  One work-group per row, four values to a lane: a block is eight lanes, a
 // scale word 32.  The row and all its partial sums are in flight at once; the row stays in registers between the two passes over it
-// (mean square, then scale and conversion).
-#define MX_NORM_T 1024
-#define MX_NORM_J 2
+// (mean square, then scale and conversion).  Squares, their sum and the normed values are held in 64 bits, which costs nothing beside
+// the loads: a value that falls on the other side of a border between two 8-bit codes is off by a step of 2^-3 to 2^-4.
 template <int NP>
 __device__ __forceinline__ float4 mx_sum_partials(float4 v, const float* p, size_t stride, int i4) {
     // the first half's sum, then the second's
@@ -144,41 +163,40 @@ __device__ __forceinline__ float4 mx_sum_partials(float4 v, const float* p, size
     return v;
 }
 
-template <int NP>
-__global__ __launch_bounds__(MX_NORM_T) void k_mx_norm(const float* h, const float* part, size_t part_stride, const float* gain, float eps, int rows,
+template <int NP, int T, int J>                              // T lanes, J groups of four columns of a lane
+__global__ __launch_bounds__(T) void k_mx_norm(const float* h, const float* part, size_t part_stride, const float* gain, float eps, int rows,
                                                       int cols, float* h_out, uint8_t* codes, uint32_t* scales) {
     const int row = blockIdx.x, n4 = cols >> 2, lane = threadIdx.x & 63;
     const size_t at = (size_t)row * cols;
-    float4 v[MX_NORM_J], g[MX_NORM_J];
-    float ss = 0.f;
+    float4 v[J], g[J];
+    double ss = 0.;
 #pragma unroll
-    for (int j = 0; j < MX_NORM_J; ++j) {
-        const int i4 = threadIdx.x + j * MX_NORM_T;
+    for (int j = 0; j < J; ++j) {
+        const int i4 = threadIdx.x + j * T;
         v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i4 < n4) {
             v[j] = ((const float4*)(h + at))[i4];
             g[j] = ((const float4*)gain)[i4];
             v[j] = mx_sum_partials<NP>(v[j], part + at, part_stride, i4);
             if (h_out && (NP > 0 || h_out != h)) ((float4*)(h_out + at))[i4] = v[j];
-            ss += v[j].x * v[j].x + v[j].y * v[j].y + v[j].z * v[j].z + v[j].w * v[j].w;
+            ss += (double)v[j].x * v[j].x + (double)v[j].y * v[j].y + (double)v[j].z * v[j].z + (double)v[j].w * v[j].w;
         }
     }
-    __shared__ float red[MX_NORM_T / 64];
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) ss += __shfl_xor(ss, s);
+    __shared__ double red[T / 64];
+    ss = mx_wave_sum(ss);
     if (lane == 0) red[threadIdx.x >> 6] = ss;
     __syncthreads();
-    float tot = 0.f;
+    double tot = 0.;
 #pragma unroll
-    for (int w = 0; w < MX_NORM_T / 64; ++w) tot += red[w];
-    const float r = 1.0f / sqrtf(tot / (float)cols + eps);
+    for (int w = 0; w < T / 64; ++w) tot += red[w];
+    const double r = 1.0 / sqrt(tot / cols + (double)eps);
     const int groups = mx_groups(cols), pad = mx_pad_rows(rows);
 #pragma unroll
-    for (int j = 0; j < MX_NORM_J; ++j) {
-        const int i4 = threadIdx.x + j * MX_NORM_T;
+    for (int j = 0; j < J; ++j) {
+        const int i4 = threadIdx.x + j * T;
         const bool in = i4 < n4;
         float y[4] = {0.f, 0.f, 0.f, 0.f};
-        if (in) { y[0] = v[j].x * r * g[j].x; y[1] = v[j].y * r * g[j].y; y[2] = v[j].z * r * g[j].z; y[3] = v[j].w * r * g[j].w; }
+        if (in) { y[0] = (float)(v[j].x * r * g[j].x); y[1] = (float)(v[j].y * r * g[j].y); y[2] = (float)(v[j].z * r * g[j].z); y[3] = (float)(v[j].w * r * g[j].w); }
         unsigned top = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = mx_max(top, __float_as_uint(y[i]) & 0x7fffffffu);
@@ -193,8 +211,9 @@ __global__ __launch_bounds__(MX_NORM_T) void k_mx_norm(const float* h, const flo
         if (!in) code = 127;
         // the word: four blocks of eight lanes
         unsigned word = code << ((lane >> 3 & 3) * 8);
-        word |= __shfl_xor(word, 8);
-        word |= __shfl_xor(word, 16);
+        word |= mx_dpp<0x140>(word);                         // the other eight of sixteen lanes, the other sixteen of 32
+        const auto halves = __builtin_amdgcn_permlane16_swap(word, word, false, false);
+        word = halves[0] | halves[1];
         const int group = i4 >> 5;
         if ((lane & 31) == 0 && group < groups) scales[(size_t)group * pad + row] = word;
         if (row == rows - 1 && group < groups && rows + (lane & 31) < pad) scales[(size_t)group * pad + rows + (lane & 31)] = 0x7f7f7f7fu;
@@ -203,8 +222,13 @@ __global__ __launch_bounds__(MX_NORM_T) void k_mx_norm(const float* h, const flo
 
 void mx_launch_norm(const float* h, const float* partials, int n_part, size_t part_stride, const float* gain, float eps, int rows, int cols,
                     float* h_out, void* codes, void* scales, hipStream_t st) {
+    // Four waves where they hold the row (2304 rows of 512 columns, one partial sum, us, sixteen waves / four: 15.4 / 5.6); longer rows
+    // take sixteen, whose loads are all in flight at once.
     auto run = [&](auto np) {
-        k_mx_norm<decltype(np)::value><<<rows, MX_NORM_T, 0, st>>>(h, partials, part_stride, gain, eps, rows, cols, h_out, (uint8_t*)codes, (uint32_t*)scales);
+        constexpr int NP = decltype(np)::value;
+        if (cols <= 1024) k_mx_norm<NP, 256, 1><<<rows, 256, 0, st>>>(h, partials, part_stride, gain, eps, rows, cols, h_out, (uint8_t*)codes, (uint32_t*)scales);
+        else if (cols <= 4096) k_mx_norm<NP, 1024, 1><<<rows, 1024, 0, st>>>(h, partials, part_stride, gain, eps, rows, cols, h_out, (uint8_t*)codes, (uint32_t*)scales);
+        else k_mx_norm<NP, 1024, 2><<<rows, 1024, 0, st>>>(h, partials, part_stride, gain, eps, rows, cols, h_out, (uint8_t*)codes, (uint32_t*)scales);
     };
     switch (n_part) {
         case 0: return run(std::integral_constant<int, 0>{});

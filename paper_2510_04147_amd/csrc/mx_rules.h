@@ -27,32 +27,31 @@ MX_HD inline int mx_slices(int K, int split) { return (K + mx_slice(K, split) - 
 // and the time of a call in us:
 //     a + b rounds over the 256 CUs + rounds x steps of 64 columns x c + share of the chip's work-groups x steps x d
 //     + weights, millions, x e + results, millions x partial sums, x f
-// d on top of c because a round that fills the chip only partly finds memory and clocks less loaded.  Fitted to 3585 calls of 18
+// d on top of c because a round that fills the chip only partly finds memory and clocks less loaded.  Fitted to 3585 timings of 18
 // matrices (512 to 37888 rows, 512 to 18944 columns), 1 to 2304 activation rows, every shape timed for each; one shape's time is met within 3 to
 // 9 % rms.  The choice is 0.6 % slower than the fastest shape on average, 4 % at the 95th percentile and 13 % at most.
 // us of some shapes by tile, weight rows x activation rows: 12288 x 4096, 32 rows 64x64 10.1, 32x32 11.5, 128x96 13.7; 160 rows 128x96 15.6, 128x128 16.6,
 // 64x64 25.8; 1000 rows 192x256 42.4, 256x256 46.0, 128x128 55.3; gate/up of 37888 x 3584, 2304 rows 256x192 241, 256x256 251, 256x128 282.
-#define MX_KINDS(X)                                                                                              \
-    X(0, 1, 1, 1, 1, 256, 4, true, false, 1, 2.6162, 0.5747, 0.0466, 0.0000, 0.0266, 1.9548)                      \
-    X(1, 2, 1, 1, 1, 256, 6, true, false, 1, 1.3974, 1.7863, 0.0587, 0.0149, 0.0429, 1.4530)                      \
-    X(2, 2, 1, 1, 2, 256, 4, true, false, 1, 1.8713, 1.6738, 0.0859, 0.0235, 0.0177, 0.9809)                      \
-    X(3, 2, 2, 1, 1, 256, 4, true, false, 1, 1.7568, 1.5940, 0.0822, 0.0214, 0.0243, 0.7856)                      \
-    X(4, 4, 1, 1, 2, 256, 4, true, false, 1, 1.9364, 1.7508, 0.1305, 0.0185, 0.0148, 0.7602)                      \
-    X(5, 4, 1, 1, 3, 256, 3, true, false, 1, 2.1455, 2.0250, 0.1460, 0.0303, 0.0015, 0.6846)                      \
-    X(6, 2, 2, 2, 2, 256, 3, true, false, 3, 1.8679, 2.7029, 0.1616, 0.0230, 0.0137, 0.6465)                      \
-    X(7, 2, 2, 4, 2, 128, 4, false, false, 3, 1.6124, 3.2137, 0.3056, 0.0079, 0.0369, 0.5122)                     \
-    X(8, 2, 2, 3, 4, 128, 3, false, false, 1, 3.1544, 3.7368, 0.3758, 0.0958, 0.0005, 0.3694)                     \
-    X(9, 2, 2, 4, 4, 128, 3, false, false, 3, 0.5452, 7.8770, 0.4636, 0.0911, 0.0060, 0.2794)                     \
-    X(10, 2, 2, 1, 2, 256, 3, true, true, 1, 2.4762, 0.9289, 0.1323, 0.0288, 0.0000, 0.7424)                      \
-    X(11, 2, 2, 2, 2, 128, 4, false, true, 1, 2.6675, 1.8194, 0.1472, 0.0920, 0.0658, 0.4508)                     \
-    X(12, 2, 2, 2, 4, 128, 3, false, true, 1, 1.5978, 5.3398, 0.3031, 0.0407, 0.0176, 0.3375)                     \
-    X(13, 1, 1, 2, 1, 256, 4, true, false, 2, 3.7295, 0.1686, 0.0684, 0.0077, 0.0423, 0.9168)                     \
-    X(14, 2, 1, 2, 1, 256, 4, true, false, 2, 1.7610, 2.1913, 0.0976, 0.0000, 0.0413, 0.9342)                     \
-    X(15, 2, 2, 2, 1, 256, 4, true, false, 2, 1.9830, 1.6215, 0.1484, 0.0000, 0.0192, 0.5291)                     \
-    X(16, 4, 1, 2, 2, 256, 3, true, false, 2, 1.9282, 3.1649, 0.1796, 0.0205, 0.0331, 0.2163)                     \
-    X(17, 2, 2, 2, 3, 256, 2, true, false, 2, 1.7230, 2.7248, 0.3026, 0.0026, 0.0084, 0.2242)                     \
-    X(18, 2, 2, 4, 3, 128, 3, false, false, 2, 0.0000, 6.4031, 0.3822, 0.0780, 0.0087, 0.0548)
-#define MX_N_KINDS 19
+#define MX_KINDS(X)                                                                                             \
+    X(0, 1, 1, 1, 1, 256, 4, true, false, 1, 2.6162, 0.5747, 0.0466, 0.0000, 0.0266, 1.9548)                    \
+    X(1, 2, 1, 1, 1, 256, 6, true, false, 1, 1.3974, 1.7863, 0.0587, 0.0149, 0.0429, 1.4530)                    \
+    X(2, 2, 2, 1, 1, 256, 4, true, false, 1, 1.7568, 1.5940, 0.0822, 0.0214, 0.0243, 0.7856)                    \
+    X(3, 4, 1, 1, 2, 256, 4, true, false, 1, 1.9364, 1.7508, 0.1305, 0.0185, 0.0148, 0.7602)                    \
+    X(4, 4, 1, 1, 3, 256, 3, true, false, 1, 2.1455, 2.0250, 0.1460, 0.0303, 0.0015, 0.6846)                    \
+    X(5, 2, 2, 2, 2, 256, 3, true, false, 3, 1.8679, 2.7029, 0.1616, 0.0230, 0.0137, 0.6465)                    \
+    X(6, 2, 2, 4, 2, 128, 4, false, false, 3, 1.6124, 3.2137, 0.3056, 0.0079, 0.0369, 0.5122)                   \
+    X(7, 2, 2, 3, 4, 128, 3, false, false, 1, 3.1544, 3.7368, 0.3758, 0.0958, 0.0005, 0.3694)                   \
+    X(8, 2, 2, 4, 4, 128, 3, false, false, 3, 0.5452, 7.8770, 0.4636, 0.0911, 0.0060, 0.2794)                   \
+    X(9, 2, 2, 1, 2, 256, 3, true, true, 1, 2.4762, 0.9289, 0.1323, 0.0288, 0.0000, 0.7424)                     \
+    X(10, 2, 2, 2, 2, 128, 4, false, true, 1, 2.6675, 1.8194, 0.1472, 0.0920, 0.0658, 0.4508)                   \
+    X(11, 2, 2, 2, 4, 128, 3, false, true, 1, 1.5978, 5.3398, 0.3031, 0.0407, 0.0176, 0.3375)                   \
+    X(12, 1, 1, 2, 1, 256, 4, true, false, 2, 3.7295, 0.1686, 0.0684, 0.0077, 0.0423, 0.9168)                   \
+    X(13, 2, 1, 2, 1, 256, 4, true, false, 2, 1.7610, 2.1913, 0.0976, 0.0000, 0.0413, 0.9342)                   \
+    X(14, 2, 2, 2, 1, 256, 4, true, false, 2, 1.9830, 1.6215, 0.1484, 0.0000, 0.0192, 0.5291)                   \
+    X(15, 4, 1, 2, 2, 256, 3, true, false, 2, 1.9282, 3.1649, 0.1796, 0.0205, 0.0331, 0.2163)                   \
+    X(16, 2, 2, 2, 3, 256, 2, true, false, 2, 1.7230, 2.7248, 0.3026, 0.0026, 0.0084, 0.2242)                   \
+    X(17, 2, 2, 4, 3, 128, 3, false, false, 2, 0.0000, 6.4031, 0.3822, 0.0780, 0.0087, 0.0548)
+#define MX_N_KINDS 18
 
 struct MxKind { int wn, wm, tn, tm, kc, nst; bool halves; int results; double t[6]; };
 inline const MxKind& mx_kind(int id) {

@@ -642,12 +642,13 @@ static int run_forward(ssd_ctx* c, const FwdHeader& hd, const int32_t* raw, int 
             {
                 ProfScope ps(c, KC_ATTN);
                 if (!(c->kernel_path >= 1 && d.dtype == SSD_BF16 &&
-                      launch_attn_mfma(c, nodes, nodes_per_seq, blen, l, fused ? ns : -1, any_suffix, st)))
+                      launch_attn_mfma(c, nodes, nodes_per_seq, blen, l, fused ? ns : -1, any_suffix, st, mx ? R : 0))) {
                     launch_attn_plain(c, R, l, st);
+                    if (mx) mx_launch_quantize(c->b.attn, SSD_BF16, R, d.nq(), SSD_MX_FP8, c->b.mx_attn, c->b.mx_attn_s, nullptr, st);
+                }
             }
             if (mx) {
-                ProfScope ps(c, KC_GEMM_O);                  // with its operand's quantisation
-                mx_launch_quantize(c->b.attn, SSD_BF16, R, d.nq(), SSD_MX_FP8, c->b.mx_attn, c->b.mx_attn_s, nullptr, st);
+                ProfScope ps(c, KC_GEMM_O);
                 gemm_mx(c, SSD_MX_OUT_F32, c->b.mx_attn, c->b.mx_attn_s, w.wo, c->b.part, nullptr, R, &ns);
             } else
                 gemm(c, KC_GEMM_O, EPI_F32, c->b.attn, w.wo, c->b.part, R, &ns);

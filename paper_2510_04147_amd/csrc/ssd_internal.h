@@ -287,6 +287,7 @@ bool launch_gemm_mfma_f32(const ssd_ctx* c, const uint16_t* x, const uint4* wp, 
 // embedding itself (nodes of at most 32 rows, head size 128, no cache append); n_part < 0: q / kown / vown are ready
 // suffix: some node of the forward sees cached positions behind its block (NodeDesc::T)
 // nodes_per_seq: nodes of every sequence of the forward if all have equally many (consecutive in the node list), else 0
+// mx_rows > 0: the output goes, microscaled in 8 bits, to mx_attn, whose scales are laid out for so many rows
 bool launch_attn_mfma(const ssd_ctx* c, int n_nodes, int nodes_per_seq, int max_blen, int layer, int n_part, bool suffix,
-                      hipStream_t st);
+                      hipStream_t st, int mx_rows = 0);
 bool attn_mfma_can_fuse_rope(const ssd_ctx* c, int max_blen);
