@@ -29,7 +29,9 @@ __device__ __forceinline__ unsigned mx_dpp(unsigned v) { return (unsigned)__buil
 __device__ __forceinline__ unsigned mx_max(unsigned a, unsigned b) { return a > b ? a : b; }
 
 // Quantisation.  A work-group of four waves takes 32 rows x 512 columns: a wave reads 512 columns of a row in one go, eight values
-// to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has the loads of its rows, every fourth, in flight together.
+// to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has its eight rows' loads in flight together.
+// They are neighbours (37888 x 3584 bf16 to 4 bits and values, us, neighbours / every fourth row: 132.6 / 135.6), but for calls of at most 32 rows, where
+// every fourth keeps all waves busy (8 x 4096: 4.1 / 3.4).
 // The tile's scale words meet in LDS and leave as whole lines.  Reads every value once: bound by memory.
 template <typename T, int BITS, bool VALUES>
 __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, int rows, int cols, uint8_t* __restrict__ codes,
@@ -38,21 +40,18 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row0 = blockIdx.x * 32, col = blockIdx.y * 512 + lane * 8;
     const bool in = col < cols;                              // whole blocks are in or out
+    const int step = rows <= 32 ? 4 : 1, first = rows <= 32 ? wave : wave * 8;
     float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int row = row0 + i * 4 + wave;
+        const int row = row0 + first + i * step;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
         if (in && row < rows) mx_load8(src + (size_t)row * cols + col, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int row = row0 + i * 4 + wave;
-        if (row >= rows) {                                   // the wave's: what only fills up
-            if ((lane & 15) == 0) words[lane >> 4][i * 4 + wave] = 0x7f7f7f7fu;
-            continue;
-        }
+        const int row = row0 + first + i * step;
         unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = mx_max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
@@ -63,7 +62,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
         if (code == 255)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-        if (in) {
+        if (in && row < rows) {
             const size_t at = (size_t)row * cols + col;
             if constexpr (BITS == 4) {
                 const unsigned o = mx_pack4(v[i], scale);
@@ -94,12 +93,12 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, 
                 }
             }
         }
-        if (!in) code = 127;                                 // what only fills up
+        if (!in || row >= rows) code = 127;                  // what only fills up
         // the word: four blocks of four lanes
         unsigned word = code << ((lane >> 2 & 3) * 8);
         word |= mx_dpp<0x141>(word);
         word |= mx_dpp<0x140>(word);
-        if ((lane & 15) == 0) words[lane >> 4][i * 4 + wave] = word;
+        if ((lane & 15) == 0) words[lane >> 4][first + i * step] = word;
     }
     __syncthreads();
     const int group = blockIdx.y * 4 + (threadIdx.x >> 5);
