@@ -75,8 +75,8 @@ __device__ __forceinline__ void mx_store4(bf16_t* p, const float* v, int left, b
 // stage has landed and with which everyone has read chunk c - 1, chunk c - 1 + NST is loaded into the stage of chunk c - 1.
 //
 // A matrix instruction takes 64 cycles, in which its wave can issue whatever is no matrix instruction: the reads of the next step's fragments
-// and the loads stand between the products one by one (160 rows of the 8B shape's gate/up 29.5 us with all of them in front of the products
-// of a step, 26.1 so; 2304 rows of the 7B class's 285 and 263).  The last step of a chunk runs behind the next barrier.
+// and the loads stand between the products one by one (160 rows of the 8B shape's gate/up in tiles of 128 x 192 29.5 us with all of them
+// in front of the products of a step, 26.1 so; 2304 rows of the 7B class's 285 and 263).  The last step of a chunk runs behind the next barrier.
 //
 // HALVES: the work-group walks two slices and adds their sums (two of four slices: what the consumer adds first).
 // A last chunk that ends inside KC runs as many steps as it has, the other half of a last half step as zeros.

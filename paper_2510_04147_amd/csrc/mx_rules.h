@@ -27,11 +27,12 @@ MX_HD inline int mx_slices(int K, int split) { return (K + mx_slice(K, split) - 
 // and the time of a call in us:
 //     a + b rounds over the 256 CUs + rounds x steps of 64 columns x c + share of the chip's work-groups x steps x d
 //     + weights, millions, x e + results, millions x partial sums, x f
-// d on top of c because a round that fills the chip only partly finds memory and clocks less loaded.  Fitted to 3585 timings of 18
+// d on top of c because a round that fills the chip only partly finds memory and clocks less loaded.  Fitted to 3605 timings of 18
 // matrices (512 to 37888 rows, 512 to 18944 columns), 1 to 2304 activation rows, every shape timed for each; one shape's time is met within 3 to
 // 9 % rms.  The choice is 0.6 % slower than the fastest shape on average, 4 % at the 95th percentile and 13 % at most.
 // us of some shapes by tile, weight rows x activation rows: 12288 x 4096, 32 rows 64x64 10.1, 32x32 11.5, 128x96 13.7; 160 rows 128x96 15.6, 128x128 16.6,
-// 64x64 25.8; 1000 rows 192x256 42.4, 256x256 46.0, 128x128 55.3; gate/up of 37888 x 3584, 2304 rows 256x192 241, 256x256 251, 256x128 282.
+// 64x64 25.8; 1000 rows 192x256 42.4, 256x256 46.0, 128x128 55.3; gate/up of 24576 x 4096, 160 rows 192x96
+// 23.1, 128x192 25.6, 256x128 28.5; of 37888 x 3584, 2304 rows 256x192 241, 256x256 251, 256x128 282.
 #define MX_KINDS(X)                                                                                             \
     X(0, 1, 1, 1, 1, 256, 4, true, false, 1, 2.6162, 0.5747, 0.0466, 0.0000, 0.0266, 1.9548)                    \
     X(1, 2, 1, 1, 1, 256, 6, true, false, 1, 1.3974, 1.7863, 0.0587, 0.0149, 0.0429, 1.4530)                    \
@@ -49,7 +50,7 @@ MX_HD inline int mx_slices(int K, int split) { return (K + mx_slice(K, split) - 
     X(13, 2, 1, 2, 1, 256, 4, true, false, 2, 1.7610, 2.1913, 0.0976, 0.0000, 0.0413, 0.9342)                   \
     X(14, 2, 2, 2, 1, 256, 4, true, false, 2, 1.9830, 1.6215, 0.1484, 0.0000, 0.0192, 0.5291)                   \
     X(15, 4, 1, 2, 2, 256, 3, true, false, 2, 1.9282, 3.1649, 0.1796, 0.0205, 0.0331, 0.2163)                   \
-    X(16, 2, 2, 2, 3, 256, 2, true, false, 2, 1.7230, 2.7248, 0.3026, 0.0026, 0.0084, 0.2242)                   \
+    X(16, 3, 1, 2, 3, 256, 3, true, false, 2, 3.2515, 2.0753, 0.2205, 0.0000, 0.0175, 0.5842)                   \
     X(17, 2, 2, 4, 3, 128, 3, false, false, 2, 0.0000, 6.4031, 0.3822, 0.0780, 0.0087, 0.0548)
 #define MX_N_KINDS 18
 

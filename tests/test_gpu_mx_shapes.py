@@ -14,12 +14,12 @@ SIZES = [(0, 5, 1, 160, "fp32"), (0, 5, 1, 160, "bf16"), (0, 2, 5, 2464, "fp32")
          (6, 135, 5429, 2144, "fp32"), (6, 604, 8512, 544, "swiglu"), (7, 1029, 7221, 96, "fp32"), (7, 1029, 7221, 96, "bf16"), (7, 263, 7367, 2080, "fp32"),
          (8, 1290, 8231, 96, "fp32"), (8, 1290, 8231, 96, "bf16"), (8, 524, 5418, 2144, "fp32"), (8, 1346, 8256, 96, "swiglu"),
          (9, 1370, 271, 2336, "fp32"), (10, 130, 4153, 2336, "fp32"), (11, 259, 5629, 2336, "fp32"), (11, 259, 5629, 2336, "bf16"),
-         (12, 2, 64, 288, "swiglu"), (13, 198, 2368, 736, "swiglu"), (14, 1, 64, 96, "swiglu"), (15, 195, 8448, 416, "swiglu"), (16, 193, 8448, 96, "swiglu"),
+         (12, 2, 64, 288, "swiglu"), (13, 198, 2368, 736, "swiglu"), (14, 1, 64, 96, "swiglu"), (15, 195, 8448, 416, "swiglu"), (15, 193, 8448, 96, "swiglu"), (16, 129, 21824, 736, "swiglu"),
          (17, 594, 8384, 96, "swiglu"),
          # several chunks and an end
          (0, 1, 1, 736, "fp32"), (1, 193, 1154, 736, "bf16"), (2, 1399, 323, 736, "fp32"), (3, 65, 8321, 736, "bf16"), (4, 195, 8197, 736, "fp32"), (5, 291, 8255, 736, "bf16"),
          (6, 386, 8297, 736, "fp32"), (7, 1544, 4877, 736, "bf16"), (8, 1286, 8067, 736, "fp32"), (5, 193, 8256, 736, "swiglu"), (6, 577, 8320, 736, "swiglu"),
-         (8, 1155, 9408, 736, "swiglu"), (14, 264, 1920, 736, "swiglu"), (15, 390, 4672, 736, "swiglu"), (16, 1220, 3136, 736, "swiglu"), (17, 897, 6592, 736, "swiglu")]
+         (8, 1155, 9408, 736, "swiglu"), (14, 264, 1920, 736, "swiglu"), (15, 390, 4672, 736, "swiglu"), (5, 1220, 3136, 736, "swiglu"), (16, 161, 24000, 1248, "swiglu"), (17, 897, 6592, 736, "swiglu")]
 
 
 def bits(o):
