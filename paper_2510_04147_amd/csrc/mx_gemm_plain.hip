@@ -1,4 +1,5 @@
-// The microscaled product, plainly: a wave per 32 x 32 outputs, operands straight from memory.
+// The microscaled product, plainly: a wave per 32 x 32 outputs, operands straight from memory.  Kernel path 0 of a context; the other kernels'
+// sums are these, bit for bit.
 #include "mx_gemm.h"
 
 // One k-slice of 32 weight rows x 32 activation rows: a chain of matrix instructions over [k0, k1).  Rows past the end read the last
@@ -57,7 +58,8 @@ __global__ __launch_bounds__(64) void k_mx_gemm_plain(MxArgs a) {
     }
 }
 
-// The sum of the partial sums, by halves.
+// The sum of the partial sums, by halves: bound by reading them, for few rows by the launch (a forward's products have no such launch:
+// the norm and the attention behind them add the sums).
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx_join(const float* __restrict__ part, int n_part, size_t stride, T* __restrict__ out, size_t n) {
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;

@@ -32,7 +32,8 @@ __device__ __forceinline__ unsigned mx_max(unsigned a, unsigned b) { return a > 
 // to a lane, so a block is four lanes and a scale word (four blocks) sixteen; a wave has its eight rows' loads in flight together.
 // They are neighbours (37888 x 3584 bf16 to 4 bits and values, us, neighbours / every fourth row: 132.6 / 135.6), but for calls of at most 32 rows, where
 // every fourth keeps all waves busy (8 x 4096: 4.1 / 3.4).
-// The tile's scale words meet in LDS and leave as whole lines.  Reads every value once: bound by memory.
+// The tile's scale words meet in LDS and leave as whole lines.  Reads every value once: bound by memory (37888 x 3584 bf16 to 4 bits 72.4 us,
+// 4.75 TB/s read and written; 4097 x 1504 fp32 to 8 bits 5.7 us, 5.4 TB/s; few rows by the launch and one trip to memory).
 template <typename T, int BITS, bool VALUES>
 __global__ __launch_bounds__(256) void k_mx_quantize(const T* __restrict__ src, int rows, int cols, uint8_t* __restrict__ codes,
                                                      uint32_t* __restrict__ scales, T* __restrict__ values) {
@@ -139,6 +140,8 @@ __device__ __forceinline__ double mx_wave_sum(double v) {
 // scale word 32.  The row and all its partial sums are in flight at once; the row stays in registers between the two passes over it
 // (mean square, then scale and conversion).  Squares, their sum and the normed values are held in 64 bits, which costs nothing beside
 // the loads: a value that falls on the other side of a border between two 8-bit codes is off by a step of 2^-3 to 2^-4.
+// Bound by memory for many rows (2304 x 3584, two partial sums, 24.7 us: 5.7 TB/s); 8 x 4096 without partial sums 3.3 us and 160 x 4096
+// with four 4.3 us are a launch, one trip to memory and the sum over the work-group.
 template <int NP>
 __device__ __forceinline__ float4 mx_sum_partials(float4 v, const float* p, size_t stride, int i4) {
     // the first half's sum, then the second's

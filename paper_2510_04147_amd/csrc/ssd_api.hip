@@ -42,7 +42,7 @@ int fail_without_ctx(int code, const char* fmt, ...) {
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    g_create_err = buf;
+    try { g_create_err = buf; } catch (...) { g_create_err.clear(); }        // no exception past a C entry
     return code;
 }
 
