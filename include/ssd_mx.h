@@ -58,7 +58,7 @@ int ssd_mx_norm(const float* h, const float* partials, int n_part, const float* 
 #define SSD_MX_OUT_SWIGLU 2   /* W = N/2 gate rows, then N/2 up rows (N a multiple of 64): silu(gate) * up in
                                  SSD_MX_FP8, out = its codes [M, N/2], out_scales = its scales                     */
 
-/* Bytes of workspace of a product (0 where it needs none, and on a bad size). */
+/* Bytes of workspace of a product (0 where it can need none, and on a bad size). */
 size_t ssd_mx_linear_workspace(int M, int N, int K, int result);
 
 /* Product: X W^T of x [M, K] in SSD_MX_FP8 and w [N, K] in SSD_MX_FP4, K a multiple of 32, on the matrix cores.  A row's result

@@ -86,6 +86,11 @@ SSD_API int ssd_mx_linear(const void* x_codes, const void* x_scales, int M, cons
     a.M = M; a.N = N; a.K = K; a.split = slices_of(N, K, result); a.st = (hipStream_t)hip_stream;
     a.out_s = (uint32_t*)out_scales;
     a.part_stride = (size_t)M * N;
+    const int all = mx_choose_all(M, N, K, a.split);
+    if (all >= 0) {
+        a.out = out;
+        return mx_gemm_all(a, all, result) ? launched(who) : fail_without_ctx(SSD_EHIP, "%s: no kernel could be set up", who);
+    }
     a.out = a.split > 1 ? workspace : out;
     int parts = 1;
     if (!mx_launch_gemm(a, a.split > 1 ? SSD_MX_OUT_F32 : result, &parts)) return fail_without_ctx(SSD_EHIP, "%s: no kernel could be set up", who);

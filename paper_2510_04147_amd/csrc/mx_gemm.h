@@ -92,8 +92,12 @@ __device__ __forceinline__ void mx_store4(bf16_t* p, const float* v, int left, b
 // HALVES: the work-group walks two slices and adds their sums (two of four slices: what the consumer adds first).
 // A last chunk that ends inside KC runs as many steps as it has, the other half of a last half step as zeros.
 // ------------------------------------------------------------------------
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
+// ALL: the waves of a work-group are the k-slices (WN = WM = TN = 1, up to four of them): each has a ring of its own and meets nobody until
+// the slices' sums do, in LDS, added as the consumers of partial sums add them; no partial sums in memory and no second launch.
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL = false>
 struct MxShape {
+    static_assert(!ALL || (WN * WM * TN == 1 && !HALVES && RESULT != SSD_MX_OUT_SWIGLU), "one wave to a slice");
+    static constexpr int WAVES = ALL ? 4 : WN * WM;
     static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, G = KC / 128, Q = KC / 64;
     static constexpr int WROW = KC / 2, XROW = KC, WP = BN * WROW / 1024, XP = BM * XROW / 1024;     // pieces of 1 KB of a chunk
     // scales: pieces of eight lines, the weights' first; every wave loads equally many pieces of each kind
@@ -102,23 +106,27 @@ struct MxShape {
     static constexpr int WJ = WP / NW, XJ = XP / NW, PER = WJ + XJ + SJ, STAGE = (WP + XP + SJ * NW) * 1024;
     static_assert(NST >= 2 && PER * (NST - 1) < 64, "ring depth");
     static constexpr int OUT = 4096;                                         // of a wave: a tile in row order
-    static constexpr int LDS = NST * STAGE > NW * OUT ? NST * STAGE : NW * OUT;
+    static constexpr int RING = NST * STAGE, LDS = ALL ? 4 * (RING > TM * OUT ? RING : TM * OUT) : RING > NW * OUT ? RING : NW * OUT;
 };
+
+// At most N of this wave's loads outstanding and none of its LDS accesses: for a ring that no other wave reads.
+template <int N>
+__device__ __forceinline__ void wait_own() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ int mx_swizzle16(int r, int pieces) { return (r / (16 / pieces)) & (pieces - 1); }
 
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
-__global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks, int m_blocks, int parts) {
-    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL>
+__global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, int n_blocks, int m_blocks, int parts) {
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
     constexpr int BN = S::BN, BM = S::BM, G = S::G, Q = S::Q, WROW = S::WROW, XROW = S::XROW, WP = S::WP, SWP = S::SWP, SXP = S::SXP;
     constexpr int NW = S::NW, STAGE = S::STAGE, XAT = WP * 1024, SAT = XAT + S::XP * 1024;           // a stage: weights, activations, scales
     constexpr int WJ = S::WJ, XJ = S::XJ, SJ = S::SJ, PER = S::PER;
     constexpr bool CHANNELS = RESULT == SSD_MX_OUT_SWIGLU;
     static_assert(!CHANNELS || TN % 2 == 0, "gate and up tiles in pairs");
     extern __shared__ uint4 smem_u4[];
-    char* const smem = (char*)smem_u4;
+    const int lane = threadIdx.x & 63, id_of_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = ALL ? 0 : id_of_wave;
+    char* const smem = (char*)smem_u4 + (ALL ? id_of_wave * S::RING : 0);    // the ring
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wm = wave / WN, lm = lane & 31, lh = lane >> 5;
 
     // Work-groups go to the 8 XCDs round-robin by their id, and every XCD has an L2 of its own: an XCD takes tiles that are neighbours
@@ -130,10 +138,10 @@ __global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks,
         const int t = xcd * per + (xcd < more ? xcd : more) + (id >> 3);
         by = t % m_blocks;
         bx = (t / m_blocks) % n_blocks;
-        bz = t / (m_blocks * n_blocks);
+        bz = ALL ? id_of_wave : t / (m_blocks * n_blocks);
     }
     const int K = a.K, k_len = mx_slice(K, a.split), spw = HALVES ? 2 : 1;
-    const int k0 = bz * spw * k_len, k1 = min(K, k0 + spw * k_len);
+    const int k0 = min(K, bz * spw * k_len), k1 = min(K, k0 + spw * k_len);  // a wave past the last slice: nothing
     const int nchunks = (k1 - k0 + KC - 1) / KC, tail = (k1 - k0) % KC;      // tail: columns of a last chunk that is not whole
     const int whole = tail ? nchunks - 1 : nchunks;
     const int boundary = HALVES ? k_len / KC : 0;
@@ -282,7 +290,11 @@ __global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks,
                 for (int m = 0; m < TM; ++m) to.sx[m] = f.sx[m];
             }
         };
-        auto landed = [&](auto bc) SSD_INLINE { wait_and_meet<PER * decltype(bc)::value>(); };        // all but the last bc chunks
+        // all but the last bc chunks
+        auto landed = [&](auto bc) SSD_INLINE {
+            if constexpr (ALL) wait_own<PER * decltype(bc)::value>();
+            else wait_and_meet<PER * decltype(bc)::value>();
+        };
         auto next_stage = [&]() SSD_INLINE {
             free = slot;
             slot = slot + 1 == NST ? 0 : slot + 1;
@@ -363,7 +375,28 @@ __global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks,
 
     // ---- results.  Lane (lm, lh) holds, per tile, weight rows 8 g + 4 lh + j of activation row lm.  They pass through LDS, where
     // every wave has an area of its own, into row order, so that a store covers whole pieces of rows.
-    __syncthreads();                                                         // the last fragments of the ring have been read
+    __syncthreads();                                                         // the last fragments of the rings have been read
+    if constexpr (ALL) {
+        using T = std::conditional_t<RESULT == SSD_MX_OUT_F32, float, bf16_t>;
+        float4* const t = (float4*)smem_u4;                                  // [slice][row tile]: 32 lines of 128 bytes, as below
+        const bool whole4 = a.N % 4 == 0;
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                t[(id_of_wave * TM + m) * 256 + lm * 8 + ((g * 2 + lh) ^ (lm & 7))] = make_float4(acc[0][m][4 * g], acc[0][m][4 * g + 1], acc[0][m][4 * g + 2], acc[0][m][4 * g + 3]);
+        __syncthreads();
+        const bool fourth = a.split > 3;                                     // three or four slices (mx_slices)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            const int r = id_of_wave * 8 + (lane >> 3), row = m0 + m * 32 + r, col = bx * 32 + (lane & 7) * 4, at = m * 256 + r * 8 + ((lane & 7) ^ (r & 7));
+            const float4 p0 = t[at], p1 = t[at + TM * 256], p2 = t[at + 2 * TM * 256], p3 = t[at + 3 * TM * 256];
+            const float v[4] = {(p0.x + p1.x) + (fourth ? p2.x + p3.x : p2.x), (p0.y + p1.y) + (fourth ? p2.y + p3.y : p2.y),
+                                (p0.z + p1.z) + (fourth ? p2.z + p3.z : p2.z), (p0.w + p1.w) + (fourth ? p2.w + p3.w : p2.w)};
+            if (row < a.M) mx_store4((T*)a.out + (size_t)row * a.N + col, v, a.N - col, whole4);
+        }
+        return;
+    }
     char* const area = smem + wave * S::OUT;
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
@@ -414,11 +447,11 @@ __global__ __launch_bounds__(WN* WM * 64) void k_mx_gemm(MxArgs a, int n_blocks,
 }
 
 // Launches one shape; *n_part = the partial sums it leaves.
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT>
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL = false>
 bool mx_launch_shape(const MxArgs& a, int* n_part) {
-    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
     static_assert(S::LDS <= 160 * 1024, "LDS budget");
-    auto kern = k_mx_gemm<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT>;
+    auto kern = k_mx_gemm<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
     static bool attr_done[64];                               // per device
     int device = 0;
     if (hipGetDevice(&device) != hipSuccess) return false;
@@ -426,10 +459,10 @@ bool mx_launch_shape(const MxArgs& a, int* n_part) {
         if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess) return false;
         if (device < 64) attr_done[device] = true;
     }
-    const int slices = mx_slices(a.K, a.split), parts = HALVES ? (slices + 1) / 2 : slices;
+    const int slices = mx_slices(a.K, a.split), parts = ALL ? 1 : HALVES ? (slices + 1) / 2 : slices;
     const int n_blocks = (a.N + S::BN - 1) / S::BN, m_blocks = (a.M + S::BM - 1) / S::BM;
     *n_part = parts;
-    kern<<<dim3((unsigned)(n_blocks * m_blocks * parts)), S::NW * 64, S::LDS, a.st>>>(a, n_blocks, m_blocks, parts);
+    kern<<<dim3((unsigned)(n_blocks * m_blocks * parts)), S::WAVES * 64, S::LDS, a.st>>>(a, n_blocks, m_blocks, parts);
     return true;
 }
 

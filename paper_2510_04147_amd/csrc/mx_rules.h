@@ -63,7 +63,7 @@ inline const MxKind& mx_kind(int id) {
 }
 
 // The shape for a call: the least estimated time, with 0.8 us for a million partial sums that the consumer reads again.
-inline int mx_choose(int M, int N, int K, int slices, bool swiglu) {
+inline int mx_choose(int M, int N, int K, int slices, bool swiglu, double* time = nullptr) {
     int best = -1;
     double least = 0;
     for (int i = 0; i < MX_N_KINDS; ++i) {
@@ -76,6 +76,38 @@ inline int mx_choose(int M, int N, int K, int slices, bool swiglu) {
         const double t = k.t[0] + k.t[1] * rounds + k.t[2] * rounds * steps + k.t[3] * wgs * steps / 256 + k.t[4] * N * K / 1e6 + k.t[5] * sums +
                          (slices > 1 ? 0.8 * sums : 0);
         if (best < 0 || t < least) { best = i; least = t; }
+    }
+    if (time) *time = least;
+    return best;
+}
+
+// A product of three or four slices whose sum is wanted, not its parts, is one launch where that is faster: a work-group of four waves per 32 weight
+// rows, each wave a slice (mx_gemm.h).  Tiles of 32 activation rows, columns of a chunk, stages, and the call's time as above, with the steps of a
+// slice.  The launch that adds partial sums takes 3 us.  Fitted to 126 calls of 14 matrices (64 to 8192 rows, 2048 to 18944 columns), 1 to 160 activation
+// rows, weights from memory: the choice is within 9 % of the faster way, 0.4 % on average.  us, one launch / two: 4096 x 4096 1 row 6.3 / 7.2, 64 rows
+// 6.7 / 10.0, 128 rows 8.7 / 13.5, 160 rows 13.9 / 12.2; 4096 x 12288 1 row 14.3 / 10.9; 8192 x 2048 64 rows 6.7 / 11.2.
+#define MX_ALL_KINDS(X)                                                 \
+    X(0, 1, 256, 2, 1.6333, 0.2987, 0.2191, 0.0000, 0.0442, 3.1069)     \
+    X(1, 2, 128, 3, 1.7476, 0.0000, 0.3106, 0.0320, 0.0191, 3.4893)
+#define MX_N_ALL_KINDS 2
+
+// Which of them a call takes, -1: none.
+inline int mx_choose_all(int M, int N, int K, int slices) {
+    if (slices < 3) return -1;
+    struct Kind { int tm; double t[6]; };
+#define MX_ALL_ROW(id, tm, kc, nst, a, b, c, d, e, f) {tm, {a, b, c, d, e, f}},
+    static const Kind kinds[MX_N_ALL_KINDS] = {MX_ALL_KINDS(MX_ALL_ROW)};
+#undef MX_ALL_ROW
+    int best = -1;
+    double least;
+    mx_choose(M, N, K, slices, false, &least);
+    least += 3;
+    for (int i = 0; i < MX_N_ALL_KINDS; ++i) {
+        const Kind& k = kinds[i];
+        const double wgs = (double)((N + 31) / 32) * ((M + 32 * k.tm - 1) / (32 * k.tm)), rounds = (double)(long long)((wgs + 255) / 256);
+        const double steps = (double)mx_slice(K, slices) / MX_STEP;
+        const double t = k.t[0] + k.t[1] * rounds + k.t[2] * rounds * steps + k.t[3] * wgs * steps / 256 + k.t[4] * N * K / 1e6 + k.t[5] * M * N / 1e6;
+        if (t < least) { best = i; least = t; }
     }
     return best;
 }

@@ -5,7 +5,7 @@ import subprocess
 
 import pytest
 
-from test_gpu_mx_shapes import SIZES
+from test_gpu_mx_shapes import ALL, SIZES
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2510_04147_amd", "csrc")
 PROGRAM = """
@@ -15,6 +15,8 @@ int split(int N, int K, int swiglu) { return mx_split(N, K, swiglu); }
 int slice(int K, int s) { return mx_slice(K, s); }
 int slices(int K, int s) { return mx_slices(K, s); }
 int choose(int M, int N, int K, int swiglu) { return mx_choose(M, N, K, mx_slices(K, mx_split(N, K, swiglu)), swiglu); }
+int choose_all(int M, int N, int K, int swiglu) { return mx_choose_all(M, N, K, mx_slices(K, mx_split(N, K, swiglu))); }
+int all_kinds() { return MX_N_ALL_KINDS; }
 int kinds() { return MX_N_KINDS; }
 int results(int k) { return mx_kind(k).results; }
 int halves(int k) { return mx_kind(k).halves; }
@@ -69,9 +71,15 @@ def test_the_gpu_tests_reach_every_shape(rules):
     reached = set()
     for kind, M, N, K, result in SIZES:
         assert rules.choose(M, N, K, int(result == "swiglu")) == kind, (kind, M, N, K, result)
-        reached.add((kind, result))
+        if rules.choose_all(M, N, K, int(result == "swiglu")) < 0:
+            reached.add((kind, result))
     for k in range(rules.kinds()):
         wanted = {"swiglu"} if rules.results(k) == 2 else {"fp32"} if rules.halves(k) else {"fp32", "bf16"}
         if rules.results(k) == 3:
             wanted.add("swiglu")
         assert wanted <= {r for kk, r in reached if kk == k}, k
+    reached = {(rules.choose_all(M, N, K, 0), result) for _, M, N, K, result in ALL}
+    assert all(rules.choose_all(M, N, K, 0) == kind for kind, M, N, K, _ in ALL)
+    assert reached == {(k, r) for k in range(rules.all_kinds()) for r in ("fp32", "bf16")}
+    assert all(rules.choose_all(M, N, K, int(N > 8192)) < 0 for M in (1, 64, 2304) for N in (64, 8192, 8256) for K in (32, 2016)) and rules.choose_all(8, 4096, 4096, 1) < 0
+    assert all(rules.choose_all(2304, N, K, 0) < 0 <= rules.choose_all(M, N, K, 0) for M in (1, 50) for N, K in ((2047, 2080), (4097, 2336), (8191, 2048), (4096, 4096)))
