@@ -224,7 +224,7 @@ __global__ __launch_bounds__(T) void k_mx_norm(const float* h, const float* part
 
 void mx_launch_norm(const float* h, const float* partials, int n_part, size_t part_stride, const float* gain, float eps, int rows, int cols,
                     float* h_out, void* codes, void* scales, hipStream_t st) {
-    // Four waves where they hold the row (2304 rows of 512 columns, one partial sum, us, sixteen waves / four: 15.4 / 5.6); longer rows
+    // Four waves where they hold the row (2304 rows of 512 columns, one partial sum, us, sixteen waves / four: 15.4 / 5.0); longer rows
     // take sixteen, whose loads are all in flight at once.
     auto run = [&](auto np) {
         constexpr int NP = decltype(np)::value;

@@ -180,9 +180,9 @@ def test_linear_not_a_number(mx):
 
 
 # ---------------------------------------------------------------- streams, graphs, workspaces
-def test_streams_and_graphs(mx):
+@pytest.mark.parametrize("M,N,K", [(40, 128, 2304), (300, 4096, 2304)])      # slices in one work-group; partial sums in the workspace
+def test_streams_and_graphs(mx, M, N, K):
     """On a stream of the caller's, captured and replayed with new operands in the same buffers, between eager calls."""
-    M, N, K = 40, 128, 2304
     st = torch.cuda.Stream()
     h = torch.empty(M, K, device="cuda")
     gain = torch.ones(K, device="cuda")
