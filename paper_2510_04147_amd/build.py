@@ -13,7 +13,8 @@ SOURCES = ["kernels_mfma.hip", "kernels_mfma_f32.hip", "gemm_f32_wn3.hip", "gemm
            "gemm_swiglu_wn3.hip", "gemm_swiglu_wn4.hip", "gemm_lmhead_wn4.hip",
            "gemm_rows_f32.hip", "gemm_rows_swiglu.hip", "gemm_rows_lmhead.hip", "ssd_api.hip", "kernels_plain.hip",
            "mx_gemm_f32.hip", "mx_gemm_f32_large.hip", "mx_gemm_bf16.hip", "mx_gemm_bf16_large.hip", "mx_gemm_swiglu.hip",
-           "mx_gemm_swiglu_large.hip", "mx_gemm_all.hip", "mx_api.hip", "mx_quantize.hip", "mx_gemm_plain.hip"]
+           "mx_gemm_swiglu_large.hip", "mx_gemm_all_f32.hip", "mx_gemm_all_bf16.hip",
+           "mx_api.hip", "mx_quantize.hip", "mx_gemm_plain.hip"]
 MEASURE_SOURCES = ["measure.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

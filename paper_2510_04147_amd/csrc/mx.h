@@ -72,7 +72,8 @@ bool mx_gemm_bf16(const MxArgs& a, int kind, int* n_part);
 bool mx_gemm_bf16_large(const MxArgs& a, int kind, int* n_part);
 bool mx_gemm_swiglu(const MxArgs& a, int kind, int* n_part);
 bool mx_gemm_swiglu_large(const MxArgs& a, int kind, int* n_part);
-// the product of three or four slices, result fp32 or bf16, in one launch (mx_choose_all's kind)
-bool mx_gemm_all(const MxArgs& a, int kind, int result);
+// the product of three or four slices in one launch (mx_choose_all's kind)
+bool mx_gemm_all_f32(const MxArgs& a, int kind);
+bool mx_gemm_all_bf16(const MxArgs& a, int kind);
 // out (bf16 or fp32, [M, N]) = the sum of the n_part partial sums, by halves
 void mx_launch_join(const float* part, int n_part, size_t part_stride, int result, void* out, size_t n, hipStream_t st);

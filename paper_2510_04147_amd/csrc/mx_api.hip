@@ -89,7 +89,7 @@ SSD_API int ssd_mx_linear(const void* x_codes, const void* x_scales, int M, cons
     const int all = mx_choose_all(M, N, K, a.split);
     if (all >= 0) {
         a.out = out;
-        return mx_gemm_all(a, all, result) ? launched(who) : fail_without_ctx(SSD_EHIP, "%s: no kernel could be set up", who);
+        return (result == SSD_MX_OUT_F32 ? mx_gemm_all_f32(a, all) : mx_gemm_all_bf16(a, all)) ? launched(who) : fail_without_ctx(SSD_EHIP, "%s: no kernel could be set up", who);
     }
     a.out = a.split > 1 ? workspace : out;
     int parts = 1;

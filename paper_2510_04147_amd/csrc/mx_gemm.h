@@ -92,10 +92,13 @@ __device__ __forceinline__ void mx_store4(bf16_t* p, const float* v, int left, b
 // HALVES: the work-group walks two slices and adds their sums (two of four slices: what the consumer adds first).
 // A last chunk that ends inside KC runs as many steps as it has, the other half of a last half step as zeros.
 // ------------------------------------------------------------------------
-// ALL: the waves of a work-group are the k-slices (WN = WM = TN = 1, up to four of them): each has a ring of its own and meets nobody until
-// the slices' sums do, in LDS, added as the consumers of partial sums add them; no partial sums in memory and no second launch.
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL = false>
+// A work-group that yields the sum of three or four slices, added as the consumers of partial sums add them, without partial sums in memory and a
+// second launch: MX_BESIDE: its waves are the slices (WN = WM = TN = 1), each with a ring of its own, and meet when the sums do, in LDS.  MX_BEHIND: it
+// walks one slice after the other and keeps the sum of those before the last two, the last but one and the one at hand in registers.
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, int JOIN = MX_APART>
 struct MxShape {
+    static constexpr bool ALL = JOIN == MX_BESIDE;
+    static_assert(JOIN == MX_APART || !HALVES, "all slices or two");
     static_assert(!ALL || (WN * WM * TN == 1 && !HALVES && RESULT != SSD_MX_OUT_SWIGLU), "one wave to a slice");
     static constexpr int WAVES = ALL ? 4 : WN * WM;
     static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32, G = KC / 128, Q = KC / 64;
@@ -115,9 +118,10 @@ __device__ __forceinline__ void wait_own() { asm volatile("s_waitcnt vmcnt(%0) l
 
 __device__ __forceinline__ int mx_swizzle16(int r, int pieces) { return (r / (16 / pieces)) & (pieces - 1); }
 
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL>
-__global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, int n_blocks, int m_blocks, int parts) {
-    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, int JOIN>
+__global__ __launch_bounds__((JOIN == MX_BESIDE ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, int n_blocks, int m_blocks, int parts) {
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, JOIN>;
+    constexpr bool ALL = S::ALL, BEHIND = JOIN == MX_BEHIND;
     constexpr int BN = S::BN, BM = S::BM, G = S::G, Q = S::Q, WROW = S::WROW, XROW = S::XROW, WP = S::WP, SWP = S::SWP, SXP = S::SXP;
     constexpr int NW = S::NW, STAGE = S::STAGE, XAT = WP * 1024, SAT = XAT + S::XP * 1024;           // a stage: weights, activations, scales
     constexpr int WJ = S::WJ, XJ = S::XJ, SJ = S::SJ, PER = S::PER;
@@ -140,11 +144,11 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
         bx = (t / m_blocks) % n_blocks;
         bz = ALL ? id_of_wave : t / (m_blocks * n_blocks);
     }
-    const int K = a.K, k_len = mx_slice(K, a.split), spw = HALVES ? 2 : 1;
+    const int K = a.K, k_len = mx_slice(K, a.split), spw = BEHIND ? a.split : HALVES ? 2 : 1;
     const int k0 = min(K, bz * spw * k_len), k1 = min(K, k0 + spw * k_len);  // a wave past the last slice: nothing
     const int nchunks = (k1 - k0 + KC - 1) / KC, tail = (k1 - k0) % KC;      // tail: columns of a last chunk that is not whole
     const int whole = tail ? nchunks - 1 : nchunks;
-    const int boundary = HALVES ? k_len / KC : 0;
+    const int boundary = HALVES || BEHIND ? k_len / KC : 0;                  // chunks of a slice
     const int F = a.N / 2, m0 = by * BM;
     // first weight row of the work-group's tile t; past the end: the last tile (never stored)
     auto tile_row = [&](int t) SSD_INLINE {
@@ -155,24 +159,37 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
             return min(bx * (BN / 32) + t, (a.N - 1) / 32) * 32;
     };
 
-    floatx16 acc[TN][TM], tot[HALVES ? TN : 1][HALVES ? TM : 1];
+    floatx16 acc[TN][TM], tot[HALVES || BEHIND ? TN : 1][HALVES || BEHIND ? TM : 1], last[BEHIND ? TN : 1][BEHIND ? TM : 1];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
         for (int m = 0; m < TM; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
+            for (int i = 0; i < 16; ++i) {
+                acc[n][m][i] = 0.f;
+                if constexpr (BEHIND) tot[n][m][i] = last[n][m][i] = 0.f;
+            }
+    int ended = 0;                                                           // slices that are done
+    // The end of a slice.  BEHIND: the slice before it joins the others, so that in front of the last slice's end `tot` is the sum of
+    // the first two and `last` the third, or with three slices in all the first and the second.  (No sum is -0: they start from 0.)
     auto flush = [&]() SSD_INLINE {
-        if constexpr (HALVES)
+        if constexpr (HALVES || BEHIND)
 #pragma unroll
             for (int n = 0; n < TN; ++n)
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
-                    tot[n][m] = acc[n][m];
+                    if constexpr (BEHIND) {
+                        tot[n][m] += last[n][m];
+                        last[n][m] = acc[n][m];
+                    } else
+                        tot[n][m] = acc[n][m];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
                 }
+        ++ended;
     };
+    // whether a slice ends in front of chunk c
+    auto ends = [&](int c) SSD_INLINE { return HALVES ? c == boundary : BEHIND && c == (ended + 1) * boundary; };
     // Fragments of a step; its scale words are those of a group, two steps: byte 0 or 2, shifted by the lane's half, is the block's.
     struct Frags { uint4 w[TN], x[TM][2]; unsigned sw[TN], sx[TM]; };
     const int fw = mx_swizzle16(lm, WROW / 16), fx = mx_swizzle16(lm, XROW / 16), shift = lh * 8;
@@ -327,7 +344,7 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
                 if (LOAD && tail && ahead == nchunks - 1) shorten();
                 next_stage();
                 step(std::integral_constant<int, 0>{}, odd, fb, all, fa, 0, load);
-                if (HALVES && c == boundary) flush();
+                if (ends(c)) flush();
                 earlier_steps(load);
                 if (LOAD) ++ahead;
                 ++c;
@@ -341,7 +358,7 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
             if (whole > 0) {
                 landed(std::integral_constant<int, 0>{});
                 next_stage();
-                if (HALVES && whole == boundary) flush();
+                if (ends(whole)) flush();
             }
             for (int q = 0; q * 64 < tail; ++q) {
                 Frags f;
@@ -362,6 +379,16 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
             }
         }
     }
+    if constexpr (BEHIND)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float t = tot[n][m][i], l = last[n][m][i], v = acc[n][m][i];
+                    acc[n][m][i] = a.split > 3 ? t + (l + v) : (t + l) + v;
+                }
     if constexpr (HALVES) {
         // one slice alone, where rounding up to chunks leaves the other one empty
         if (k1 - k0 > k_len)
@@ -447,11 +474,11 @@ __global__ __launch_bounds__((ALL ? 4 : WN * WM) * 64) void k_mx_gemm(MxArgs a, 
 }
 
 // Launches one shape; *n_part = the partial sums it leaves.
-template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, bool ALL = false>
+template <int WN, int WM, int TN, int TM, int KC, int NST, int RESULT, bool HALVES, bool NT, int JOIN = MX_APART>
 bool mx_launch_shape(const MxArgs& a, int* n_part) {
-    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
+    using S = MxShape<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, JOIN>;
     static_assert(S::LDS <= 160 * 1024, "LDS budget");
-    auto kern = k_mx_gemm<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, ALL>;
+    auto kern = k_mx_gemm<WN, WM, TN, TM, KC, NST, RESULT, HALVES, NT, JOIN>;
     static bool attr_done[64];                               // per device
     int device = 0;
     if (hipGetDevice(&device) != hipSuccess) return false;
@@ -459,7 +486,7 @@ bool mx_launch_shape(const MxArgs& a, int* n_part) {
         if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess) return false;
         if (device < 64) attr_done[device] = true;
     }
-    const int slices = mx_slices(a.K, a.split), parts = ALL ? 1 : HALVES ? (slices + 1) / 2 : slices;
+    const int slices = mx_slices(a.K, a.split), parts = JOIN != MX_APART ? 1 : HALVES ? (slices + 1) / 2 : slices;
     const int n_blocks = (a.N + S::BN - 1) / S::BN, m_blocks = (a.M + S::BM - 1) / S::BM;
     *n_part = parts;
     kern<<<dim3((unsigned)(n_blocks * m_blocks * parts)), S::WAVES * 64, S::LDS, a.st>>>(a, n_blocks, m_blocks, parts);
@@ -476,5 +503,16 @@ bool mx_launch_kind(const MxArgs& a, int kind, int* n_part) {
         if (kind == id) return mx_launch_shape<wn, wm, tn, tm, kc, nst, RESULT, halves, nt>(a, n_part);
     MX_KINDS(MX_KIND_CASE)
 #undef MX_KIND_CASE
+    return false;
+}
+
+// The same for the shapes with all slices in a work-group.
+template <int RESULT>
+bool mx_launch_all(const MxArgs& a, int kind) {
+    int parts;
+#define MX_ALL_CASE(id, wn, wm, tn, tm, kc, nst, nt, join, ...) \
+    if (kind == id) return mx_launch_shape<wn, wm, tn, tm, kc, nst, RESULT, false, nt, join>(a, &parts);
+    MX_ALL_KINDS(MX_ALL_CASE)
+#undef MX_ALL_CASE
     return false;
 }

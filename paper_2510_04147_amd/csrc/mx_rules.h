@@ -81,31 +81,40 @@ inline int mx_choose(int M, int N, int K, int slices, bool swiglu, double* time 
     return best;
 }
 
-// A product of three or four slices whose sum is wanted, not its parts, is one launch where that is faster: a work-group of four waves per 32 weight
-// rows, each wave a slice (mx_gemm.h).  Tiles of 32 activation rows, columns of a chunk, stages, and the call's time as above, with the steps of a
-// slice.  The launch that adds partial sums takes 3 us.  Fitted to 126 calls of 14 matrices (64 to 8192 rows, 2048 to 18944 columns), 1 to 160 activation
-// rows, weights from memory: the choice is within 9 % of the faster way, 0.4 % on average.  us, one launch / two: 4096 x 4096 1 row 6.3 / 7.2, 64 rows
-// 6.7 / 10.0, 128 rows 8.7 / 13.5, 160 rows 13.9 / 12.2; 4096 x 12288 1 row 14.3 / 10.9; 8192 x 2048 64 rows 6.7 / 11.2.
-#define MX_ALL_KINDS(X)                                                 \
-    X(0, 1, 256, 2, 1.6333, 0.2987, 0.2191, 0.0000, 0.0442, 3.1069)     \
-    X(1, 2, 128, 3, 1.7476, 0.0000, 0.3106, 0.0320, 0.0191, 3.4893)
-#define MX_N_ALL_KINDS 2
+// A product of three or four slices whose sum is wanted, not its parts, is one launch where that is faster (mx_gemm.h): slices beside each other, a
+// work-group of four waves per 32 weight rows and each wave a slice, for few rows; slices behind each other, for many.  id, as above but for the
+// result, MX_BESIDE or MX_BEHIND, and the call's time as above, with the steps of a slice or of all of them.  The launch that adds partial
+// sums takes 3.5 us and 0.03 for a million outputs.  Fitted to 126 calls of 14 matrices (64 to 8192 rows, 2048 to 18944 columns), 1 to 160
+// activation rows, and 195 of 13, 64 to 4000 rows, weights from memory.  The choice is 0.4 % slower than the fastest way on average, 19 % at most.
+// us, one launch / two: 4096 x 4096 1 row 6.3 / 7.2, 64 rows 6.7 / 10.0, 500 rows 13.6 / 19.7, 1000 rows 21.2 / 29.8, 2304 rows 59.5 / 70.7;
+// 4096 x 12288 1 row 14.3 / 10.9, 1000 rows 54.5 / 56.5; 8192 x 2048 64 rows 6.7 / 11.2, 2304 rows 65.9 / 99.5.
+// Slices behind each other have tiles of at most 128 rows (three sets of sums are all that registers hold), so they read the activations more often:
+// not where the L2s do not hold them (4000 x 2080 x 8224 161 / 120 us).
+enum { MX_APART, MX_BESIDE, MX_BEHIND };
+#define MX_ALL_KINDS(X)                                                                                          \
+    X(0, 1, 1, 1, 1, 256, 2, true, MX_BESIDE, 1.6333, 0.2987, 0.2191, 0.0000, 0.0442, 3.1069)                    \
+    X(1, 1, 1, 1, 2, 128, 3, true, MX_BESIDE, 1.7476, 0.0000, 0.3106, 0.0320, 0.0191, 3.4893)                    \
+    X(2, 2, 2, 1, 1, 256, 4, false, MX_BEHIND, 1.3649, 2.2618, 0.0941, 0.0148, 0.0000, 0.1919)                   \
+    X(3, 4, 1, 1, 2, 256, 4, false, MX_BEHIND, 1.1710, 3.3180, 0.1316, 0.0210, 0.0047, 0.0494)                   \
+    X(4, 2, 2, 2, 2, 256, 3, false, MX_BEHIND, 0.0914, 5.7895, 0.1891, 0.0536, 0.0165, 0.0511)
+#define MX_N_ALL_KINDS 5
 
 // Which of them a call takes, -1: none.
 inline int mx_choose_all(int M, int N, int K, int slices) {
     if (slices < 3) return -1;
-    struct Kind { int tm; double t[6]; };
-#define MX_ALL_ROW(id, tm, kc, nst, a, b, c, d, e, f) {tm, {a, b, c, d, e, f}},
+    struct Kind { int bn, bm, join; double t[6]; };
+#define MX_ALL_ROW(id, wn, wm, tn, tm, kc, nst, nt, join, a, b, c, d, e, f) {wn * tn * 32, wm * tm * 32, join, {a, b, c, d, e, f}},
     static const Kind kinds[MX_N_ALL_KINDS] = {MX_ALL_KINDS(MX_ALL_ROW)};
 #undef MX_ALL_ROW
     int best = -1;
     double least;
     mx_choose(M, N, K, slices, false, &least);
-    least += 3;
+    least += 3.5 + 0.03e-6 * M * N;
     for (int i = 0; i < MX_N_ALL_KINDS; ++i) {
         const Kind& k = kinds[i];
-        const double wgs = (double)((N + 31) / 32) * ((M + 32 * k.tm - 1) / (32 * k.tm)), rounds = (double)(long long)((wgs + 255) / 256);
-        const double steps = (double)mx_slice(K, slices) / MX_STEP;
+        if (k.join == MX_BEHIND && (double)M * K > 1 << 24) continue;
+        const double wgs = (double)((N + k.bn - 1) / k.bn) * ((M + k.bm - 1) / k.bm), rounds = (double)(long long)((wgs + 255) / 256);
+        const double steps = (double)(k.join == MX_BESIDE ? mx_slice(K, slices) : K) / MX_STEP;
         const double t = k.t[0] + k.t[1] * rounds + k.t[2] * rounds * steps + k.t[3] * wgs * steps / 256 + k.t[4] * N * K / 1e6 + k.t[5] * M * N / 1e6;
         if (t < least) { best = i; least = t; }
     }

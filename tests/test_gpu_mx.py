@@ -180,7 +180,7 @@ def test_linear_not_a_number(mx):
 
 
 # ---------------------------------------------------------------- streams, graphs, workspaces
-@pytest.mark.parametrize("M,N,K", [(40, 128, 2304), (300, 4096, 2304)])      # slices in one work-group; partial sums in the workspace
+@pytest.mark.parametrize("M,N,K", [(40, 128, 2304), (300, 4096, 2304), (9000, 130, 2304)])      # slices beside and behind each other; partial sums in the workspace
 def test_streams_and_graphs(mx, M, N, K):
     """On a stream of the caller's, captured and replayed with new operands in the same buffers, between eager calls."""
     st = torch.cuda.Stream()

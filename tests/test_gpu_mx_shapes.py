@@ -20,12 +20,14 @@ SIZES = [(0, 5, 1, 160, "fp32"), (0, 5, 1, 160, "bf16"), (0, 2, 5, 2464, "fp32")
          (0, 1, 1, 736, "fp32"), (1, 193, 1154, 736, "bf16"), (2, 1399, 323, 736, "fp32"), (3, 65, 8321, 736, "bf16"), (4, 195, 8197, 736, "fp32"), (5, 291, 8255, 736, "bf16"),
          (6, 386, 8297, 736, "fp32"), (7, 1544, 4877, 736, "bf16"), (8, 1286, 8067, 736, "fp32"), (5, 193, 8256, 736, "swiglu"), (6, 577, 8320, 736, "swiglu"),
          (8, 1155, 9408, 736, "swiglu"), (14, 264, 1920, 736, "swiglu"), (15, 390, 4672, 736, "swiglu"), (5, 1220, 3136, 736, "swiglu"), (16, 161, 24000, 1248, "swiglu"), (17, 897, 6592, 736, "swiglu"),
-         # three slices, two of them joined by the kernel
-         (9, 67, 5465, 2336, "fp32"), (10, 130, 5465, 2336, "fp32")]
+         # three and four slices, two of them joined by the kernel, partial sums by another
+         (9, 5000, 130, 4128, "fp32"), (10, 8000, 130, 2336, "fp32"), (11, 8000, 324, 2336, "fp32")]
 # Products whose slices share a work-group: kind (mx_choose_all), rows, weight rows, columns, result; three and four slices, ends inside a
 # chunk and inside a step, rows of outputs that are no multiple of four, rows past a tile
-ALL = [(0, 1, 4096, 4096, "bf16"), (0, 1, 33, 2048, "fp32"), (0, 5, 65, 2304, "bf16"), (0, 31, 2047, 2080, "fp32"), (0, 32, 8191, 2048, "bf16"), (0, 65, 4097, 2336, "fp32"),
-       (0, 7, 1, 3104, "bf16"), (0, 1039, 75, 2400, "bf16"), (1, 33, 4097, 2336, "bf16"), (1, 64, 8191, 2048, "fp32"), (1, 129, 2047, 2080, "bf16"), (1, 37, 8190, 4128, "fp32")]
+ALL = [(0, 1, 4096, 4096, "bf16"), (0, 1, 33, 2048, "fp32"), (0, 5, 65, 2304, "bf16"), (0, 31, 2047, 2080, "fp32"), (0, 32, 8191, 2048, "bf16"), (2, 65, 4097, 2336, "fp32"),
+       (0, 7, 1, 3104, "bf16"), (0, 1039, 75, 2400, "bf16"), (1, 33, 4097, 2336, "bf16"), (1, 64, 8191, 2048, "fp32"), (1, 129, 2047, 2080, "bf16"), (2, 37, 8190, 4128, "fp32"),
+       (2, 300, 2047, 2080, "bf16"), (3, 131, 5465, 2336, "bf16"), (3, 300, 4097, 2336, "fp32"), (4, 257, 6532, 2336, "bf16"), (4, 1000, 4096, 4096, "fp32"),
+       (4, 524, 5418, 2144, "fp32")]
 
 
 def bits(o):
@@ -62,19 +64,19 @@ def test_shape(kind, M, N, K, result):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows", [1, 50])
+@pytest.mark.parametrize("rows", [1, 50, 300, 1000, 2304])
 @pytest.mark.parametrize("N,K", [(2047, 2080), (4097, 2336), (8191, 2048), (4096, 4096)])
 def test_slices_in_a_work_group_equal_slices_apart(rows, N, K):
-    """A few rows, whose slices share a work-group, against the same rows among 2304, whose partial sums a second kernel adds."""
+    """Rows whose slices share a work-group against the same rows among 9000, whose partial sums a second kernel adds."""
     from paper_2510_04147_amd import mx
     g = torch.Generator().manual_seed(N + K + rows)
     w = mx.quantize((torch.randn(N, K, generator=g) * 0.02).cuda(), mx.FP4)
     x = torch.randn(rows, K, generator=g).cuda()
-    many = x.repeat(2304 // rows + 1, 1)[:2304].contiguous()
+    many = x.repeat(9000 // rows + 1, 1)[:9000].contiguous()
     for result in ("fp32", "bf16"):
         few = mx.linear(mx.quantize(x, mx.FP8), w, result)
         among = mx.linear(mx.quantize(many, mx.FP8), w, result)
-        assert torch.equal(among[:rows], few) and torch.equal(among[2304 // rows * rows - rows:2304 // rows * rows], few)
+        assert torch.equal(among[:rows], few) and torch.equal(among[9000 // rows * rows - rows:9000 // rows * rows], few)
 
 
 @pytest.mark.gpu

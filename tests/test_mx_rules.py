@@ -82,4 +82,4 @@ def test_the_gpu_tests_reach_every_shape(rules):
     assert all(rules.choose_all(M, N, K, 0) == kind for kind, M, N, K, _ in ALL)
     assert reached == {(k, r) for k in range(rules.all_kinds()) for r in ("fp32", "bf16")}
     assert all(rules.choose_all(M, N, K, int(N > 8192)) < 0 for M in (1, 64, 2304) for N in (64, 8192, 8256) for K in (32, 2016)) and rules.choose_all(8, 4096, 4096, 1) < 0
-    assert all(rules.choose_all(2304, N, K, 0) < 0 <= rules.choose_all(M, N, K, 0) for M in (1, 50) for N, K in ((2047, 2080), (4097, 2336), (8191, 2048), (4096, 4096)))
+    assert all(rules.choose_all(9000, N, K, 0) < 0 <= rules.choose_all(M, N, K, 0) for M in (1, 50, 300, 1000, 2304) for N, K in ((2047, 2080), (4097, 2336), (8191, 2048), (4096, 4096)))
