@@ -19,6 +19,7 @@ from . import binding
 FP4, FP8 = 4, 8
 OUT_F32, OUT_BF16, OUT_SWIGLU = range(3)
 RESULTS = {"fp32": OUT_F32, "bf16": OUT_BF16, "swiglu": OUT_SWIGLU}
+_MOST = (1 << 31) - 1                                   # of a C int, which ctypes would fill with the low bits of a larger number
 EXPORTS = ["ssd_mx_scale_bytes", "ssd_mx_quantize", "ssd_mx_norm", "ssd_mx_linear_workspace", "ssd_mx_linear"]
 
 _lib = None
@@ -76,6 +77,10 @@ def _call(index, f, *args):
         raise binding.SsdError(rc, _lib.ssd_strerror(rc).decode(), _lib.ssd_last_error(None).decode())
 
 
+def _beyond(who, *sizes):
+    return binding.SsdError(-2, _lib.ssd_strerror(-2).decode(), f"{who}: {' x '.join(map(str, sizes))} is beyond the supported size")
+
+
 def scale_shape(rows, cols):
     return ((cols + 127) // 128, (rows + 31) // 32 * 32, 4)
 
@@ -95,6 +100,8 @@ def quantize(x, bits, values=None, out=None):
     rows, cols = shape
     if rows < 1 or cols < 1 or cols % 32:
         raise _bad(x, "a matrix with columns in blocks of 32")
+    if rows > _MOST or cols > _MOST:
+        raise _beyond("ssd_mx_quantize", rows, cols)
     if bits != FP4 and bits != FP8:
         raise ValueError(f"bits must be 4 or 8, got {bits}")
     if out is None:
@@ -115,6 +122,8 @@ def norm(h, partials, gain, eps, h_out=None, out=None, keep=True):
     if partials is not None:
         n = partials.shape[0] if partials.dim() == 3 else -1
         parts = _operand(partials, index, f32, (n, rows, cols))
+    if rows > _MOST or cols > _MOST or n > _MOST:
+        raise _beyond("ssd_mx_norm", n, rows, cols)
     if out is None:
         out = empty(rows, cols, FP8, h.device)
     at = _operand(h, index, f32, shape)
@@ -137,6 +146,8 @@ def linear(x, w, result="bf16", out=None, workspace=None):
     if N < 1 or (kind == OUT_SWIGLU and N % 64):
         raise ValueError(f"rows of weights are needed, gate and up rows in blocks of 32, got {N}")
     M, K = shape
+    if M > _MOST or N > _MOST or K > _MOST:
+        raise _beyond("ssd_mx_linear", M, N, K)
     xc, xs = _matrix(x, index, M, K, FP8)
     wc, ws = _matrix(w, index, N, K, FP4)
     if kind == OUT_SWIGLU:
@@ -162,5 +173,5 @@ def linear(x, w, result="bf16", out=None, workspace=None):
 
 
 def linear_workspace(M, N, K, result="bf16"):
-    """Bytes of workspace of linear()."""
-    return lib().ssd_mx_linear_workspace(M, N, K, RESULTS[result])
+    """Bytes of workspace of linear(); 0 where it needs none, and on a bad size."""
+    return 0 if max(M, N, K) > _MOST or min(M, N, K) < 1 else lib().ssd_mx_linear_workspace(M, N, K, RESULTS[result])
