@@ -208,6 +208,11 @@ class SSD:
         if rc != 0:
             raise SsdError(rc, self.lib.ssd_strerror(rc).decode(), self.lib.ssd_last_error(None).decode())
         self.h = h
+        if self.ccfg.dtype == SSD_MXFP4:
+            # the context has 4-bit copies of the projections once the stream gets here and reads only the other weights again: the
+            # caller's projections end with the caller's own references
+            self.stream.synchronize()
+            self.weights = {**weights, "layers": [{n: lw[n] for n in ("norm1", "norm2")} for lw in weights["layers"]]}
 
     def close(self):
         if getattr(self, "h", None):
