@@ -13,6 +13,8 @@
  *           ssd_mx_scale_bytes(rows, cols) bytes.  Rows and blocks that only fill up hold 127; readers pay no heed to them.
  * The scale of a block is the smallest power of two for which its largest value, rounded, is not past the largest
  * element: every value is off by at most half a step of the element's format.  An infinity or a NaN makes its block NaN.
+ * (Producers that take the exponent of the largest value as it is, and saturate, give a block whose largest is in [7, 8) times a power
+ * of two, with 8 bits in (464, 512), half this scale.  Such matrices are read like any other; their codes are not these.)
  *
  * Conventions: those of ssd.h (return codes, host-side validation, nothing launched by a call that fails).  All pointers
  * are device pointers; the calls need no context, run asynchronously on `hip_stream` (NULL = the default stream) and
@@ -56,9 +58,12 @@ int ssd_mx_norm(const float* h, const float* partials, int n_part, const float* 
 #define SSD_MX_OUT_F32    0   /* out fp32 [M, N]                                                                  */
 #define SSD_MX_OUT_BF16   1   /* out bf16 [M, N]                                                                  */
 #define SSD_MX_OUT_SWIGLU 2   /* W = N/2 gate rows, then N/2 up rows (N a multiple of 64): silu(gate) * up in
-                                 SSD_MX_FP8, out = its codes [M, N/2], out_scales = its scales                     */
+                                 SSD_MX_FP8, out = its codes [M, N/2], out_scales = its scales; silu is 0 for
+                                 gates below about -87, where 1 / (1 + e^-gate) ends among the normal floats        */
 
-/* Bytes of workspace of a product (0 where it can need none, and on a bad size). */
+/* Bytes of workspace of a product: the partial sums of all k-slices of its matrix (0 where that has one slice, and on a bad
+ * size).  Proportional to M: a workspace for the most rows serves every call with fewer.  Calls that add their slices in
+ * one launch, a matter of speed, leave it as it is. */
 size_t ssd_mx_linear_workspace(int M, int N, int K, int result);
 
 /* Product: X W^T of x [M, K] in SSD_MX_FP8 and w [N, K] in SSD_MX_FP4, K a multiple of 32, on the matrix cores.  A row's result

@@ -135,7 +135,7 @@ def norm(h, partials, gain, eps, h_out=None, out=None, keep=True):
 def linear(x, w, result="bf16", out=None, workspace=None):
     """x (8 bits, [M, K]) times w (4 bits, [N, K]) transposed.  result "bf16" or "fp32": a tensor [M, N]; "swiglu": w holds gate
     rows, then up rows, and the result is silu(gate) * up as (codes, scales) of 8 bits, [M, N / 2].  workspace: a uint8 tensor of at
-    least linear_workspace(...) bytes, else one is allocated where the product needs it."""
+    least linear_workspace(...) bytes, else one is allocated where the matrix has several k-slices."""
     l, kind = lib(), RESULTS.get(result)
     if kind is None:
         raise ValueError(f"result must be one of {sorted(RESULTS)}, got {result!r}")
@@ -173,5 +173,5 @@ def linear(x, w, result="bf16", out=None, workspace=None):
 
 
 def linear_workspace(M, N, K, result="bf16"):
-    """Bytes of workspace of linear(); 0 where it needs none, and on a bad size."""
+    """Bytes of workspace of linear(): proportional to M; 0 where the matrix has one k-slice, and on a bad size."""
     return 0 if max(M, N, K) > _MOST or min(M, N, K) < 1 else lib().ssd_mx_linear_workspace(M, N, K, RESULTS[result])

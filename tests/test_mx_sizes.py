@@ -60,3 +60,12 @@ def test_workspace_of_a_product_beyond_the_sizes():
     assert mx.linear_workspace(8, 64, 4096) > 0
     for M, N, K in ((BIG, 64, 4096), (8, BIG * 64, 4096), (8, 64, BIG * 1024), (8 - (1 << 32), 64, 4096)):
         assert mx.linear_workspace(M, N, K) == 0
+
+
+@pytest.mark.parametrize("N,K", [(64, 2304), (512, 4096), (4096, 4096), (8192, 2048), (8192, 18944)])
+def test_a_workspace_for_the_most_rows_serves_fewer(N, K):
+    """Whichever kernels the row counts take."""
+    one = mx.linear_workspace(1, N, K)
+    assert one > 0
+    for M in (2, 33, 160, 1000, 9000):
+        assert mx.linear_workspace(M, N, K) == mx.linear_workspace(M, N, K, "fp32") == M * one
