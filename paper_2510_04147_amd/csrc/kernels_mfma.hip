@@ -473,8 +473,10 @@ __global__ __launch_bounds__(SHARED ? 256 : 512, 2) void k_attn_mfma(const FwdHe
         o[e] = acc * inv;
     }
     if constexpr (MX) {
-        // bf16 as without MX, then 8 bits and a scale for every block of 32 head channels.  The merge spreads a block over 16 / EPW
-        // waves: their maxima meet where the query tile lay.  A kernel of its own for this costs 4 us a layer.
+        // bf16 as without MX, then 8 bits and a scale for every block of 32 head channels.  bf16 first so that both kernel paths and the
+        // operators called one by one (attention, then quantisation) give the same codes: one value in 32 is rounded to a tie of the 8-bit
+        // grid and lands on the other neighbour, off by 2^-9 of its size more than the half step of 2^-4.  The merge spreads a block over
+        // 16 / EPW waves: their maxima meet where the query tile lay.  A kernel of its own for this costs 4 us a layer.
         constexpr int PER_BLOCK = 16 / EPW;
         unsigned(*const tops)[32] = (unsigned(*)[32])&qs[0][0];
         unsigned top = 0;

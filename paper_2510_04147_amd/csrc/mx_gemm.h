@@ -24,6 +24,8 @@ __device__ __forceinline__ mx_floatx16 mx_mfma(uint4 w, uint4 x0, uint4 x1, unsi
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 0, BYTE, (int)sw, BYTE, (int)sx);
 }
 
+// silu(g) u, within (|g| + 4) 2^-23 of its size (the exponent |g| log2 e is rounded twice), finer than the sums that it is given; 0 below
+// about -87, where the reciprocal is no normal float.
 __device__ __forceinline__ float mx_silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
 // Activated channels of 32 channels x 32 rows (gate and up sums of one tile each) as e4m3 codes and one scale per row.  Lane (lm,
@@ -81,13 +83,16 @@ __device__ __forceinline__ void mx_store4(bf16_t* p, const float* v, int left, b
 // stage has landed and with which everyone has read chunk c - 1, chunk c - 1 + NST is loaded into the stage of chunk c - 1.
 //
 // A matrix instruction takes 64 cycles, in which its wave can issue whatever is no matrix instruction: the reads of the next step's fragments
-// and the loads stand between the products one by one (160 rows of the 8B shape's gate/up in tiles of 128 x 192 29.5 us with all of them
-// in front of the products of a step, 26.1 so; 2304 rows of the 7B class's 285 and 263).  The last step of a chunk runs behind the next barrier.
+// and the loads stand between the products one by one (160 rows of the 8B shape's gate/up in tiles of 192 x 96 27.0 us with all of them
+// in front of the products of a step, 24.7 so; 2304 rows of the 7B class's, 256 x 192, 302 and 278; both in turn on one card).  The last step of
+// a chunk runs behind the next barrier.
 //
 // What bounds it, by rows: up to 32 the weights' stream (12288 x 4096 in 10 us, 2.8 TB/s: the launch, the first chunks' way from memory and
 // the sums' way back are half of it); 64 to 300 the requests of a CU, a cache line of weights taking 5.3 ns and one of activations,
-// which the L2 holds, 1.2 ns (24576 x 4096, 160 rows: 23 us, of which the matrix instructions and barriers alone take 15, with the reads of
-// LDS 17.4); thousands the matrix cores (37888 x 3584, 2304 rows: 241 us, 2.6 PFLOP/s, where the instruction alone reaches 3.5 on such codes).
+// which the L2 holds, 1.2 ns (24576 x 4096, 160 rows, 192 x 96: 22 to 25 us by card; where it took 23 the matrix instructions and barriers alone
+// took 15, with the reads of LDS 17.4.  Its two row blocks fetch every line of weights twice and cover 192 rows, and its three waves leave a SIMD
+// of every CU without matrix instructions); thousands the matrix cores (37888 x 3584, 2304 rows: 237 to 279 us by card and load before it,
+// 2.2 to 2.6 PFLOP/s, where the instruction alone reaches 3.5 on such codes).
 //
 // HALVES: the work-group walks two slices and adds their sums (two of four slices: what the consumer adds first).
 // A last chunk that ends inside KC runs as many steps as it has, the other half of a last half step as zeros.

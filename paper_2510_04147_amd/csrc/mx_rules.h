@@ -30,9 +30,10 @@ MX_HD inline int mx_slices(int K, int split) { return (K + mx_slice(K, split) - 
 // d on top of c because a round that fills the chip only partly finds memory and clocks less loaded.  Fitted to 3605 timings of 18
 // matrices (512 to 37888 rows, 512 to 18944 columns), 1 to 2304 activation rows, every shape timed for each; one shape's time is met within 3 to
 // 9 % rms.  The choice is 0.6 % slower than the fastest shape on average, 4 % at the 95th percentile and 13 % at most.
-// us of some shapes by tile, weight rows x activation rows: 12288 x 4096, 32 rows 64x64 10.1, 32x32 11.5, 128x96 13.7; 160 rows 128x96 15.6, 128x128 16.6,
-// 64x64 25.8; 1000 rows 192x256 42.4, 256x256 46.0, 128x128 55.3; gate/up of 24576 x 4096, 160 rows 192x96
-// 23.1, 128x192 25.6, 256x128 28.5; of 37888 x 3584, 2304 rows 256x192 241, 256x256 251, 256x128 282.
+// us of some shapes by tile, weight rows x activation rows, in turn on one card: 12288 x 4096, 32 rows 64x32 9.8, 64x64 10.7,
+// 32x32 11.0, 128x96 13.9; 160 rows 128x96 17.4, 128x128 20.0, 64x64 27.9; 1000 rows 192x256 52.1, 256x256 55.7, 128x128 66.6; gate/up of
+// 24576 x 4096, 32 rows 128x32 13.4, 64x32 15.0, 128x64 15.2; 160 rows 192x96 24.7, 256x128 33.0, 256x64 35.6; of 37888 x 3584, 2304 rows
+// 256x192 278, 256x256 279, 256x128 310.
 #define MX_KINDS(X)                                                                                             \
     X(0, 1, 1, 1, 1, 256, 4, true, false, 1, 2.6162, 0.5747, 0.0466, 0.0000, 0.0266, 1.9548)                    \
     X(1, 2, 1, 1, 1, 256, 6, true, false, 1, 1.3974, 1.7863, 0.0587, 0.0149, 0.0429, 1.4530)                    \
@@ -88,8 +89,11 @@ inline int mx_choose(int M, int N, int K, int slices, bool swiglu, double* time 
 // activation rows, and 195 of 13, 64 to 4000 rows, weights from memory.  The choice is 0.4 % slower than the fastest way on average, 19 % at most.
 // us, one launch / two: 4096 x 4096 1 row 6.3 / 7.2, 64 rows 6.7 / 10.0, 500 rows 13.6 / 19.7, 1000 rows 21.2 / 29.8, 2304 rows 59.5 / 70.7;
 // 4096 x 12288 1 row 14.3 / 10.9, 1000 rows 54.5 / 56.5; 8192 x 2048 64 rows 6.7 / 11.2, 2304 rows 65.9 / 99.5.
-// Slices behind each other have tiles of at most 128 rows (three sets of sums are all that registers hold), so they read the activations more often:
-// not where the L2s do not hold them (4000 x 2080 x 8224 161 / 120 us).
+// Slices behind each other have tiles of at most 128 rows (three sets of sums are all that registers hold), so they read the activations more often.
+// The times were fitted to activations of no more than the L2s hold, and past M K = 2^24 the slices stay apart.  Measured past it (up to 50 M values,
+// 512 to 8192 weight rows; behind each other / apart, ratio by columns): 2080 0.46 to 0.84, 4096 0.62 to 0.83, 8192 0.74 to 1.05, 12288 0.89 to 1.26: at
+// 12288 columns the border is right, with fewer it costs the calls of many rows (us, 10082 x 8192 x 2080 310 / 603, 8192 x 4096 x 4096 190 / 285,
+// 6144 x 4096 x 8192 253 / 277, 4096 x 4096 x 12288 251 / 217).
 enum { MX_APART, MX_BESIDE, MX_BEHIND };
 #define MX_ALL_KINDS(X)                                                                                          \
     X(0, 1, 1, 1, 1, 256, 2, true, MX_BESIDE, 1.6333, 0.2987, 0.2191, 0.0000, 0.0442, 3.1069)                    \
